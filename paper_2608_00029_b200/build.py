@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libnova_attn.so")
 SOURCES = ["api.cu", "attn_fwd.cu", "attn_bwd.cu", "attn_bwd_pre.cu", "attn_dq.cu", "attn_dq64.cu", "attn_dkdv.cu", "attn_dkdv64.cu",
-           "attn_bwd_static.cu", "lmhead.cu", "lmhead_rows.cu"]
+           "attn_bwd_static.cu", "lmhead.cu", "lmhead_rows.cu", "ops/rope.cu", "ops/window_api.cu", "ops/window_decode.cu"]
 BINDING = os.path.join(HERE, "_binding.so")
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared", "-cudart", "shared", "-Xlinker", "-soname=libnova_attn.so"]
@@ -32,9 +32,8 @@ def _stale() -> bool:
         if f"nova binding for {_built_for()}\0".encode() not in f.read():
             return True
     t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
-    deps = _sources() + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh", ".cpp"))]
-    deps.append(os.path.join(os.path.dirname(HERE), "include", "nova_attn.h"))
-    deps.append(os.path.join(os.path.dirname(HERE), "include", "nova_lmhead.h"))
+    deps = _sources() + [os.path.join(d, f) for d in (CSRC, os.path.join(CSRC, "ops"), os.path.join(os.path.dirname(HERE), "include"))
+                         for f in os.listdir(d) if f.endswith((".h", ".cuh", ".cpp"))]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

@@ -12,6 +12,7 @@
 
 #include "../../include/nova_attn.h"
 #include "../../include/nova_lmhead.h"
+#include "api.h"
 #include "kernels.h"
 #include "work_plan.h"
 
@@ -33,12 +34,6 @@ using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t
                                    CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 constexpr int kMaxDevices = 64;
-struct DeviceState {
-    bool ready = false;
-    int status = NOVA_ATTN_OK;  // sticky result of the one-time set-up
-    int num_sms = 0;
-    int* dev_status = nullptr;
-};
 std::mutex g_mutex;
 DeviceState g_devices[kMaxDevices];
 // Test aid (nova_attn_test_configure_waits): cycle limit of the device-side waits and the fault to inject.
@@ -47,8 +42,8 @@ std::atomic<long long> g_wait_limit{kDefaultWaitLimit};
 std::atomic<int> g_inject{0};
 EncodeTiledFn g_encode = nullptr;
 
-// One-time set-up of the current device: capability check, opt-in shared memory sizes, address of
-// the device status word, tensor-map encoder entry point.
+}  // namespace
+
 int device_state(DeviceState** out) {
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -89,6 +84,8 @@ int device_state(DeviceState** out) {
     *out = &st;
     return NOVA_ATTN_OK;
 }
+
+namespace {
 
 // Tensor maps are pure functions of (pointer, shape, strides); a small cache keeps the host cost of a
 // call to a lookup when the same buffers are used step after step.
@@ -230,25 +227,26 @@ int check_lmhead_shape(int M, int N, int K) {
     return NOVA_ATTN_OK;
 }
 
-// Heads and batches of the tensor merge into one dimension (the [B,H,T,D] family): 3-D maps, plain kernels.
+}  // namespace
+
 bool merges(const AttnShape& s, const TensorStrides& st) {
     return st.b == static_cast<long long>(s.H) * st.h && st.t <= st.h;
 }
 
-// The map of a bf16 tensor for the plain (3-D) or the strided (4-D) build of the kernels.
 int get_bf16_map(const void* ptr, const AttnShape& s, const TensorStrides& st, bool strided, CUtensorMap* out,
-                 uint32_t* order, int box_rows = kBlockQ) {
+                 uint32_t* order, int box_rows) {
     if (strided) return get_tensor_map4(ptr, s, st, out, order, box_rows);
     *order = 0;
     return get_tensor_map(ptr, s.D, s.T, static_cast<long long>(s.B) * s.H, out, 2, st.t, st.h, box_rows);
 }
 
+namespace {
 TensorStrides contiguous_strides(int H, int T, int D) {
     return TensorStrides{static_cast<long long>(H) * T * D, static_cast<long long>(T) * D, static_cast<long long>(D)};
 }
 
-// Strides are in elements; every one a multiple of 8 (16 bytes, which TMA and the 16-byte accesses of the
-// helper kernels need), the token stride at least D, none so large that a byte offset leaves 2^40.
+}  // namespace
+
 int check_strides(const nova_attn_strides* p, int D, TensorStrides* out) {
     if (!p) return NOVA_ATTN_ERR_NULL;
     if ((p->batch & 7) || (p->head & 7) || (p->token & 7)) return NOVA_ATTN_ERR_ALIGNMENT;
@@ -259,11 +257,13 @@ int check_strides(const nova_attn_strides* p, int D, TensorStrides* out) {
     return NOVA_ATTN_OK;
 }
 
+namespace {
 // Workspace of the backward: the fp32 dQ accumulator [B,H,T,D], rounded up to 256 bytes.
 size_t acc_bytes(int B, int H, int T, int D) {
     const size_t n = static_cast<size_t>(B) * H * T * D * sizeof(float);
     return (n + 255) & ~size_t(255);
 }
+}  // namespace
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
@@ -276,8 +276,6 @@ int check_shape(int B, int H, int T, int D) {
     if (bh > (1ll << 30) || bh * tiles > 2147483647ll || static_cast<long long>(T) > (1ll << 30)) return NOVA_ATTN_ERR_SHAPE;
     return NOVA_ATTN_OK;
 }
-
-}  // namespace
 
 int record_cuda_error(int code) { return fail_cuda(code); }
 
@@ -351,7 +349,7 @@ int nova_attn_bwd_preprocess_strided(const void* O, const void* dO, float* Delta
     if (int rc = device_state(&st)) return rc;
     const AttnShape s{B, H, T, D, 1, 1.f};
     const cudaError_t e =
-        launch_attn_bwd_preprocess(static_cast<const __nv_bfloat16*>(O), static_cast<const __nv_bfloat16*>(dO), Delta, s,
+        launch_attn_bwd_preprocess(static_cast<const __nv_bfloat16*>(O), nullptr, static_cast<const __nv_bfloat16*>(dO), Delta, s,
                                    so, sdo, st->num_sms, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? NOVA_ATTN_OK : fail_cuda(e);
 }

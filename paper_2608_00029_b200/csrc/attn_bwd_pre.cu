@@ -1,5 +1,6 @@
 // Memory-bound helpers of the backward pass.
-//   bwd_preprocess_kernel: Delta_i = sum_d dO[i,d] * O[i,d]   (row term of the softmax Jacobian)
+//   bwd_preprocess_kernel: Delta_i = sum_d dO[i,d] * O[i,d]   (row term of the softmax Jacobian), with what rounding took from
+//                          O beside it if the caller has it (kRest)
 //   dq_convert_kernel:     dQ = bf16(scale * fp32 accumulator)
 //   zero_kernel:           clears the fp32 accumulator before the backward kernel adds into it
 // Both stream their inputs once with 16-byte loads; rows are split over D/8 lanes and reduced with
@@ -62,9 +63,10 @@ __device__ __forceinline__ long long row_offset16(long long r, const RowSplit& r
 }
 
 // LPR = lanes per row = D/8 (8 for D=64, 16 for D=128); each lane owns 8 consecutive bf16.
-template <int LPR, int UNROLL, bool kContiguous>
-__global__ void __launch_bounds__(256) bwd_preprocess_kernel(const uint4* __restrict__ O, const uint4* __restrict__ dO,
-                                                             float* __restrict__ Delta, long long rows, const RowSplit rs,
+template <int LPR, int UNROLL, bool kContiguous, bool kRest>
+__global__ void __launch_bounds__(256) bwd_preprocess_kernel(const uint4* __restrict__ O, const uint4* __restrict__ rest,
+                                                             const uint4* __restrict__ dO, float* __restrict__ Delta,
+                                                             long long rows, const RowSplit rs,
                                                              const TensorStrides so, const TensorStrides sdo) {
     griddep_launch_dependents();
     griddep_wait();
@@ -74,11 +76,13 @@ __global__ void __launch_bounds__(256) bwd_preprocess_kernel(const uint4* __rest
     const int sub = static_cast<int>(tid % LPR);
     long long r = tid / LPR;
     for (; r < rows; r += rows_per_pass * UNROLL) {
-        uint4 a[UNROLL], b[UNROLL];
+        uint4 a[UNROLL], b[UNROLL], c[kRest ? UNROLL : 1];
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             const long long ru = r + u * rows_per_pass;
+            if constexpr (kRest) c[u] = make_uint4(0, 0, 0, 0);
             if (ru < rows) {
+                if constexpr (kRest) c[u] = __ldg(rest + (kContiguous ? ru * LPR : row_offset16(ru, rs, so)) + sub);
                 a[u] = __ldg(O + (kContiguous ? ru * LPR : row_offset16(ru, rs, so)) + sub);
                 b[u] = __ldg(dO + (kContiguous ? ru * LPR : row_offset16(ru, rs, sdo)) + sub);
             } else {
@@ -89,6 +93,7 @@ __global__ void __launch_bounds__(256) bwd_preprocess_kernel(const uint4* __rest
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             float acc = dot8_bf16(a[u], b[u]);
+            if constexpr (kRest) acc += dot8_bf16(c[u], b[u]);
 #pragma unroll
             for (int off = LPR / 2; off > 0; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
             const long long ru = r + u * rows_per_pass;
@@ -107,9 +112,10 @@ __global__ void __launch_bounds__(256) bwd_preprocess_kernel(const uint4* __rest
 // B=4, H=32, T=1000, D=128, against 5.5 and 9.4 us here (inputs in L2); from DRAM 16.4 and 24.6 against 14.3 and 21.4.
 __host__ __device__ constexpr int tok_tile(int D, int heads, int batches) { return batches * 4 * (2048 / D) / heads; }
 
-template <int LPR, int kTokHeads, int kBatches>
-__global__ void __launch_bounds__(256, 4) bwd_preprocess_tokens_kernel(const uint4* __restrict__ O, const uint4* __restrict__ dO,
-                                                                    float* __restrict__ Delta, int H, int T, int t_tiles,
+template <int LPR, int kTokHeads, int kBatches, bool kRest>
+__global__ void __launch_bounds__(256, 4) bwd_preprocess_tokens_kernel(const uint4* __restrict__ O, const uint4* __restrict__ rest,
+                                                                    const uint4* __restrict__ dO, float* __restrict__ Delta,
+                                                                    int H, int T, int t_tiles,
                                                                     int h_tiles, const TensorStrides so,
                                                                     const TensorStrides sdo) {
     constexpr int kRowsPerPass = 256 / LPR, kPasses = 4, kTokTile = tok_tile(8 * LPR, kTokHeads, kBatches);
@@ -121,15 +127,18 @@ __global__ void __launch_bounds__(256, 4) bwd_preprocess_tokens_kernel(const uin
     const int sub = threadIdx.x % LPR, row0 = threadIdx.x / LPR;
     const uint4* po = O + ((b * so.b) >> 3) + sub;
     const uint4* pd = dO + ((b * sdo.b) >> 3) + sub;
+    const uint4* pr = rest + ((b * so.b) >> 3) + sub;
     griddep_wait();
 #pragma unroll
     for (int p = 0; p < kBatches * kPasses; p += kPasses) {
-        uint4 x[kPasses], y[kPasses];
+        uint4 x[kPasses], y[kPasses], z[kRest ? kPasses : 1];
 #pragma unroll
         for (int u = 0; u < kPasses; ++u) {
             const int r = row0 + (p + u) * kRowsPerPass, t = t0 + r / kTokHeads, h = h0 + r % kTokHeads;
             x[u] = y[u] = make_uint4(0, 0, 0, 0);
+            if constexpr (kRest) z[u] = x[u];
             if (t < T && h < H) {
+                if constexpr (kRest) z[u] = __ldg(pr + ((h * so.h + t * so.t) >> 3));
                 x[u] = __ldg(po + ((h * so.h + t * so.t) >> 3));
                 y[u] = __ldg(pd + ((h * sdo.h + t * sdo.t) >> 3));
             }
@@ -137,6 +146,7 @@ __global__ void __launch_bounds__(256, 4) bwd_preprocess_tokens_kernel(const uin
 #pragma unroll
         for (int u = 0; u < kPasses; ++u) {
             float acc = dot8_bf16(x[u], y[u]);
+            if constexpr (kRest) acc += dot8_bf16(z[u], y[u]);
 #pragma unroll
             for (int off = LPR / 2; off > 0; off >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, off);
             const int r = row0 + (p + u) * kRowsPerPass;
@@ -220,9 +230,11 @@ bool is_contiguous(const AttnShape& s, const TensorStrides& st) {
 }
 }  // namespace
 
-cudaError_t launch_attn_bwd_preprocess(const __nv_bfloat16* O, const __nv_bfloat16* dO, float* Delta,
-                                       const AttnShape& s, const TensorStrides& so, const TensorStrides& sdo,
-                                       int num_sms, cudaStream_t stream) {
+namespace {
+template <bool kRest>
+cudaError_t launch_preprocess(const __nv_bfloat16* O, const __nv_bfloat16* rest, const __nv_bfloat16* dO, float* Delta,
+                              const AttnShape& s, const TensorStrides& so, const TensorStrides& sdo, int num_sms,
+                              cudaStream_t stream) {
     constexpr int kThreads = 256, kUnroll = 4;
     const long long rows = static_cast<long long>(s.B) * s.H * s.T;
     const int lpr = s.D / 8;
@@ -233,6 +245,7 @@ cudaError_t launch_attn_bwd_preprocess(const __nv_bfloat16* O, const __nv_bfloat
     if (blocks < 1) blocks = 1;
     const uint4* o4 = reinterpret_cast<const uint4*>(O);
     const uint4* d4 = reinterpret_cast<const uint4*>(dO);
+    const uint4* r4 = reinterpret_cast<const uint4*>(rest);
     const dim3 grid(static_cast<unsigned>(blocks));
     const bool contiguous = is_contiguous(s, so) && is_contiguous(s, sdo);
     if (!contiguous && so.h < so.t && sdo.h < sdo.t) {
@@ -245,28 +258,37 @@ cudaError_t launch_attn_bwd_preprocess(const __nv_bfloat16* O, const __nv_bfloat
         const int tile = tok_tile(s.D, heads, batches), t_tiles = (s.T + tile - 1) / tile, h_tiles = (s.H + heads - 1) / heads;
         const long long blocks_tok = static_cast<long long>(s.B) * t_tiles * h_tiles;
         auto go = [&](auto kernel) {
-            return launch_overlapped(kernel, dim3(static_cast<unsigned>(blocks_tok)), dim3(kThreads), 0, stream, o4, d4, Delta,
+            return launch_overlapped(kernel, dim3(static_cast<unsigned>(blocks_tok)), dim3(kThreads), 0, stream, o4, r4, d4, Delta,
                                      s.H, s.T, t_tiles, h_tiles, so, sdo);
         };
         if (blocks_tok <= 0x7fffffff) {
             if (s.D == 64)
-                return heads == 8   ? go(bwd_preprocess_tokens_kernel<8, 8, 1>)
-                       : heads == 4 ? go(bwd_preprocess_tokens_kernel<8, 4, 1>)
-                                    : go(bwd_preprocess_tokens_kernel<8, 2, 1>);
+                return heads == 8   ? go(bwd_preprocess_tokens_kernel<8, 8, 1, kRest>)
+                       : heads == 4 ? go(bwd_preprocess_tokens_kernel<8, 4, 1, kRest>)
+                                    : go(bwd_preprocess_tokens_kernel<8, 2, 1, kRest>);
             if (batches == 1)
-                return heads == 8   ? go(bwd_preprocess_tokens_kernel<16, 8, 1>)
-                       : heads == 4 ? go(bwd_preprocess_tokens_kernel<16, 4, 1>)
-                                    : go(bwd_preprocess_tokens_kernel<16, 2, 1>);
-            return heads == 8   ? go(bwd_preprocess_tokens_kernel<16, 8, 2>)
-                   : heads == 4 ? go(bwd_preprocess_tokens_kernel<16, 4, 2>)
-                                : go(bwd_preprocess_tokens_kernel<16, 2, 2>);
+                return heads == 8   ? go(bwd_preprocess_tokens_kernel<16, 8, 1, kRest>)
+                       : heads == 4 ? go(bwd_preprocess_tokens_kernel<16, 4, 1, kRest>)
+                                    : go(bwd_preprocess_tokens_kernel<16, 2, 1, kRest>);
+            return heads == 8   ? go(bwd_preprocess_tokens_kernel<16, 8, 2, kRest>)
+                   : heads == 4 ? go(bwd_preprocess_tokens_kernel<16, 4, 2, kRest>)
+                                : go(bwd_preprocess_tokens_kernel<16, 2, 2, kRest>);
         }
     }
     auto go = [&](auto kernel) {
-        return launch_overlapped(kernel, grid, dim3(kThreads), 0, stream, o4, d4, Delta, rows, split_of(s), so, sdo);
+        return launch_overlapped(kernel, grid, dim3(kThreads), 0, stream, o4, r4, d4, Delta, rows, split_of(s), so, sdo);
     };
-    if (s.D == 64) return contiguous ? go(bwd_preprocess_kernel<8, kUnroll, true>) : go(bwd_preprocess_kernel<8, kUnroll, false>);
-    return contiguous ? go(bwd_preprocess_kernel<16, kUnroll, true>) : go(bwd_preprocess_kernel<16, kUnroll, false>);
+    if (s.D == 64)
+        return contiguous ? go(bwd_preprocess_kernel<8, kUnroll, true, kRest>) : go(bwd_preprocess_kernel<8, kUnroll, false, kRest>);
+    return contiguous ? go(bwd_preprocess_kernel<16, kUnroll, true, kRest>) : go(bwd_preprocess_kernel<16, kUnroll, false, kRest>);
+}
+}  // namespace
+
+cudaError_t launch_attn_bwd_preprocess(const __nv_bfloat16* O, const __nv_bfloat16* rest, const __nv_bfloat16* dO, float* Delta,
+                                       const AttnShape& s, const TensorStrides& so, const TensorStrides& sdo,
+                                       int num_sms, cudaStream_t stream) {
+    return rest != nullptr ? launch_preprocess<true>(O, rest, dO, Delta, s, so, sdo, num_sms, stream)
+                           : launch_preprocess<false>(O, rest, dO, Delta, s, so, sdo, num_sms, stream);
 }
 
 cudaError_t launch_dq_convert(const float* dq_acc, __nv_bfloat16* dQ, const AttnShape& s, const TensorStrides& sdq,

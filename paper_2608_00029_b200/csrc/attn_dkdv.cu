@@ -63,11 +63,18 @@ struct KvBars {
 };
 static_assert(sizeof(KvBars) <= 512, "barrier block");
 
-// Work items: 128-key tiles; heads in chunks, heaviest tiles first within a chunk.
+// Work items: 128-key tiles; heads in chunks, heaviest tiles first within a chunk.  kWindow: the heads are those of K and V, and an
+// item has the steps of all query heads that share its head, one after another.
+template <bool kWindow>
 struct KvWork {
     int BH, n_tiles, chunk, T, H;
     uint32_t orders;  // coordinate orders of the Q, K, V, dO, dK, dV tensor maps, four bits each
     bool causal;
+    Window win;
+    // Steps of one query head in an item of n.
+    __device__ __forceinline__ int per_head(int kt, int n) const {
+        return kWindow ? query_steps(win, kt * kBlockK, kBlockK, T, kStep) : n;
+    }
     // Key tile, head, first step and number of steps of item `idx`.
     __device__ __forceinline__ void get(int idx, int* kt, int* bh, int* s0, int* n) const {
         const int per_chunk = chunk * n_tiles;
@@ -76,13 +83,14 @@ struct KvWork {
         *kt = in / heads;
         *bh = ck * chunk + in - *kt * heads;
         *s0 = causal ? *kt * (kBlockK / kStep) : 0;
-        *n = (T + kStep - 1) / kStep - *s0;
+        *n = kWindow ? win.group * query_steps(win, *kt * kBlockK, kBlockK, T, kStep) : (T + kStep - 1) / kStep - *s0;
     }
 };
 
-template <bool kStrided>
+template <bool kStrided, bool kWindow>
 __device__ __forceinline__ void kv_producer(const CUtensorMap* tmQ, const CUtensorMap* tmK, const CUtensorMap* tmV,
-                                            const CUtensorMap* tmdO, uint8_t* smem, KvBars* bars, const KvWork& wk) {
+                                            const CUtensorMap* tmdO, uint8_t* smem, KvBars* bars,
+                                            const KvWork<kWindow>& wk) {
     volatile int* abort_flag = &bars->abort_flag;
     int armed_k[2] = {-1, -1}, armed_v = -1, armed_q[kQStages];
     for (int s = 0; s < kQStages; ++s) armed_q[s] = -1;
@@ -105,6 +113,8 @@ __device__ __forceinline__ void kv_producer(const CUtensorMap* tmQ, const CUtens
         for (int h = 0; h < kHalves; ++h)
             tma_load_tile<kStrided>(smem + kOffK + ks * kTileBytes + h * kHalfTileBytes, tmK, &bars->k_full[ks],
                                     (wk.orders >> 4) & 15, h * kBoxCols, kt * kBlockK, head, batch, bh);
+        const int per = wk.per_head(kt, n);
+        int q_head = kWindow ? head * wk.win.group : head, q_bh = kWindow ? bh * wk.win.group : bh, sh = 0;
         for (int s = 0; s < n; ++s) {
             ok = mbar_wait(&bars->q_empty[st], ph ^ 1, abort_flag);
             if (!ok) break;
@@ -113,9 +123,14 @@ __device__ __forceinline__ void kv_producer(const CUtensorMap* tmQ, const CUtens
 #pragma unroll
             for (int h = 0; h < kHalves; ++h) {
                 tma_load_tile<kStrided>(smem + kOffQ + st * kStepBytes + h * kHalfStepBytes, tmQ, &bars->q_full[st],
-                                        wk.orders & 15, h * kBoxCols, (s0 + s) * kStep, head, batch, bh);
+                                        wk.orders & 15, h * kBoxCols, (s0 + sh) * kStep, q_head, batch, q_bh);
                 tma_load_tile<kStrided>(smem + kOffdO + st * kStepBytes + h * kHalfStepBytes, tmdO, &bars->q_full[st],
-                                        (wk.orders >> 12) & 15, h * kBoxCols, (s0 + s) * kStep, head, batch, bh);
+                                        (wk.orders >> 12) & 15, h * kBoxCols, (s0 + sh) * kStep, q_head, batch, q_bh);
+            }
+            if (++sh == per) {  // on to the next query head
+                sh = 0;
+                ++q_head;
+                ++q_bh;
             }
             if (++st == kQStages) {
                 st = 0;
@@ -153,7 +168,8 @@ __device__ __forceinline__ void kv_producer(const CUtensorMap* tmQ, const CUtens
 }
 
 // UMMA issuer: the whole warp in uniform control flow, one elected lane issues.
-__device__ __forceinline__ void kv_mma(uint8_t* smem, KvBars* bars, uint32_t tmem_base, const KvWork& wk) {
+template <bool kWindow>
+__device__ __forceinline__ void kv_mma(uint8_t* smem, KvBars* bars, uint32_t tmem_base, const KvWork<kWindow>& wk) {
     volatile int* abort_flag = &bars->abort_flag;
     constexpr uint32_t kIdescT = umma_idesc_bf16(128, kStep, 0, 0);  // S^T, dP^T
     constexpr uint32_t kIdescKV = umma_idesc_bf16(128, D, 0, 1);     // dV, dK: A from TMEM, B MN-major
@@ -304,8 +320,9 @@ __device__ __forceinline__ void kv_mma(uint8_t* smem, KvBars* bars, uint32_t tme
 // sum, so that it reaches no key behind it.  (Making what is masked zero in the compute warps, per packed word or in a
 // branch that is not taken, cost 0.8 to 1.5 % of the training pass at B=4, H=32, T=1000.)  The loads of four steps are in
 // flight together.
+template <bool kWindow>
 __device__ __forceinline__ void kv_row_loader(KvBars* bars, float* row_buf, const float* __restrict__ LSE,
-                                              const float* __restrict__ Delta, const KvWork& wk, int lane) {
+                                              const float* __restrict__ Delta, const KvWork<kWindow>& wk, int lane) {
     volatile int* abort_flag = &bars->abort_flag;
     constexpr int kDeep = 4;
     int g = 0;
@@ -314,17 +331,25 @@ __device__ __forceinline__ void kv_row_loader(KvBars* bars, float* row_buf, cons
         if (item < 0) return;
         int kt, bh, s0, n;
         wk.get(item, &kt, &bh, &s0, &n);
-        const size_t base = static_cast<size_t>(bh) * wk.T;
+        const int per = wk.per_head(kt, n), last = kWindow ? (bh + 1) * wk.win.group - 1 : bh;
+        int q_bh = kWindow ? bh * wk.win.group : bh, sh = 0;
         for (int s = 0; s < n; s += kDeep) {
             float l[kDeep][2], d[kDeep][2];
 #pragma unroll
-            for (int u = 0; u < kDeep; ++u)
+            for (int u = 0; u < kDeep; ++u) {
+                const size_t base = static_cast<size_t>(q_bh) * wk.T;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const int q = (s0 + s + u) * kStep + lane + 32 * x;
+                    const int q = (s0 + sh) * kStep + lane + 32 * x;
                     l[u][x] = (q < wk.T) ? LSE[base + q] : INFINITY;
                     d[u][x] = (q < wk.T) ? Delta[base + q] : 0.f;
                 }
+                ++sh;
+                if (kWindow && sh == per) {  // (what is loaded past the item's last step is not used)
+                    sh = 0;
+                    q_bh = min(q_bh + 1, last);
+                }
+            }
 #pragma unroll
             for (int u = 0; u < kDeep; ++u) {
                 if (s + u >= n) break;
@@ -346,9 +371,9 @@ __device__ __forceinline__ void kv_row_loader(KvBars* bars, float* row_buf, cons
 }
 
 // Compute group `grp` (steps g with g % 2 == grp, which are those of buffer `grp`), warp `cwarp` of it.
-template <bool kCausal>
+template <bool kCausal, bool kWindow>
 __device__ __forceinline__ void kv_compute(const uint8_t* smem, KvBars* bars, uint32_t tmem_base, float scale,
-                                           const KvWork& wk, int grp, int cwarp, int lane) {
+                                           const KvWork<kWindow>& wk, int grp, int cwarp, int lane) {
     volatile int* abort_flag = &bars->abort_flag;
     const uint32_t lane_base = 32u * cwarp;
     const int r = lane_base + lane;  // local key row
@@ -368,7 +393,11 @@ __device__ __forceinline__ void kv_compute(const uint8_t* smem, KvBars* bars, ui
         int kt, bh, s0, n;
         wk.get(item, &kt, &bh, &s0, &n);
         const int key = kt * kBlockK + r;
-        for (int s = (g ^ grp) & 1; s < n; s += 2) {
+        const int per = wk.per_head(kt, n);
+        int sh = (g ^ grp) & 1;  // the step in its query head
+        for (int s = (g ^ grp) & 1; s < n; s += 2, sh += 2) {
+            if constexpr (kWindow)
+                while (sh >= per) sh -= per;
             const int gs = g + s;
             const int rb = gs % kRowStages;
             ok = mbar_wait(&bars->row_full[rb], (gs / kRowStages) & 1, abort_flag);
@@ -378,8 +407,9 @@ __device__ __forceinline__ void kv_compute(const uint8_t* smem, KvBars* bars, ui
             const float4* l4 = reinterpret_cast<const float4*>(row_buf + rb * 2 * kStep);
             const float4* d4 = l4 + kStep / 4;
             // Keep key <= query.  Keys past the end of the sequence need no mask: their rows are not stored.
-            const bool masked = kCausal && s < kBlockK / kStep;
+            const bool masked = kWindow ? any_dropping(wk.win, kt * kBlockK, (s0 + sh) * kStep) : kCausal && s < kBlockK / kStep;
             const int first = key - (s0 + s) * kStep;  // first kept query of the step
+            const uint64_t kept = kWindow ? keeping_queries(wk.win, key, (s0 + sh) * kStep) : 0ull;
             // Half a step at a time, rolled: the two groups are at different places of this loop.
 #pragma unroll 1
             for (int q = 0; q < kStep; q += 32) {
@@ -388,9 +418,10 @@ __device__ __forceinline__ void kv_compute(const uint8_t* smem, KvBars* bars, ui
                 tmem_ld_x32(t_dp + q, dv);
                 tmem_wait_ld();
                 if (masked) {
+                    const uint32_t kept32 = static_cast<uint32_t>(kept >> q);
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
-                        if (q + i < first) sv[i] = 0xff800000u;  // -inf: P = 0
+                        if (kWindow ? !(kept32 >> i & 1u) : q + i < first) sv[i] = 0xff800000u;  // -inf: P = 0
                 }
 #pragma unroll
                 for (int i = 0; i < 32; i += 4) {
@@ -443,9 +474,9 @@ __device__ __forceinline__ void kv_stage_row(uint8_t* stage, int r, const uint32
 
 // Write-out warps (warp `owarp` of four, thread = key row): dV, then dK * scale, of a finished item as bf16 into the item's K
 // buffer and out with TMA stores, while the compute warps are in the next item.
-template <bool kStrided>
+template <bool kStrided, bool kWindow>
 __device__ __forceinline__ void kv_write_out(uint8_t* smem, KvBars* bars, uint32_t tmem_base, const CUtensorMap* tmdK,
-                                             const CUtensorMap* tmdV, float scale, const KvWork& wk, int owarp, int lane) {
+                                             const CUtensorMap* tmdV, float scale, const KvWork<kWindow>& wk, int owarp, int lane) {
     volatile int* abort_flag = &bars->abort_flag;
     const uint32_t lane_base = 32u * owarp;
     const int r = lane_base + lane;
@@ -525,13 +556,13 @@ __device__ __forceinline__ void kv_write_out(uint8_t* smem, KvBars* bars, uint32
     if (leader) bulk_wait_group<0>();  // dV and dK must be complete before the kernel ends
 }
 
-template <bool kCausal, bool kStrided>
+template <bool kCausal, bool kStrided, bool kWindow>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_dkdv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                  const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmdO,
                  const __grid_constant__ CUtensorMap tmdK, const __grid_constant__ CUtensorMap tmdV,
                  const float* __restrict__ LSE, const float* __restrict__ Delta, int T, int BH, int H, uint32_t orders,
-                 int n_tiles, int chunk, float scale, int* __restrict__ dev_status) {
+                 int n_tiles, int chunk, float scale, int* __restrict__ dev_status, const Window win) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     if (smem != smem_raw) {
@@ -543,7 +574,7 @@ attn_dkdv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     }
     KvBars* bars = reinterpret_cast<KvBars*>(smem + kOffBar);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const KvWork wk{BH, n_tiles, chunk, T, H, orders, kCausal};
+    const KvWork<kWindow> wk{BH, n_tiles, chunk, T, H, orders, kCausal, win};
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < 2; ++s) {
@@ -589,15 +620,15 @@ attn_dkdv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     griddep_wait();  // everything above overlaps the previous kernel of the stream
 
     if (warp == 0) {
-        if (lane == 0) kv_producer<kStrided>(&tmQ, &tmK, &tmV, &tmdO, smem, bars, wk);
+        if (lane == 0) kv_producer<kStrided, kWindow>(&tmQ, &tmK, &tmV, &tmdO, smem, bars, wk);
     } else if (warp == 1) {
         kv_mma(smem, bars, tmem_base, wk);
     } else if (warp == 2) {
         kv_row_loader(bars, reinterpret_cast<float*>(smem + kOffRow), LSE, Delta, wk, lane);
     } else if (warp >= 12) {
-        kv_write_out<kStrided>(smem, bars, tmem_base, &tmdK, &tmdV, scale, wk, warp & 3, lane);
+        kv_write_out<kStrided, kWindow>(smem, bars, tmem_base, &tmdK, &tmdV, scale, wk, warp & 3, lane);
     } else if (warp >= 4) {
-        kv_compute<kCausal>(smem, bars, tmem_base, scale, wk, (warp - 4) >> 2, warp & 3, lane);
+        kv_compute<kCausal, kWindow>(smem, bars, tmem_base, scale, wk, (warp - 4) >> 2, warp & 3, lane);
     }
 
     tc_fence_before();
@@ -612,26 +643,47 @@ cudaError_t configure_attn_dkdv() {
     auto set = [](auto kernel) {
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
     };
-    cudaError_t e = set(attn_dkdv_kernel<true, false>);
-    if (e == cudaSuccess) e = set(attn_dkdv_kernel<true, true>);
-    if (e == cudaSuccess) e = set(attn_dkdv_kernel<false, false>);
-    if (e == cudaSuccess) e = set(attn_dkdv_kernel<false, true>);
+    cudaError_t e = set(attn_dkdv_kernel<true, false, false>);
+    if (e == cudaSuccess) e = set(attn_dkdv_kernel<true, true, false>);
+    if (e == cudaSuccess) e = set(attn_dkdv_kernel<false, false, false>);
+    if (e == cudaSuccess) e = set(attn_dkdv_kernel<false, true, false>);
+    if (e == cudaSuccess) e = set(attn_dkdv_kernel<true, false, true>);
+    if (e == cudaSuccess) e = set(attn_dkdv_kernel<true, true, true>);
     return e;
 }
+
+namespace {
+// BH: heads of K and V in all, H: in a sequence.
+cudaError_t launch_dkdv(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
+                        const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided, uint32_t orders, const float* LSE,
+                        const float* Delta, const AttnShape& s, int H, const Window* win, int num_sms, int* dev_status,
+                        cudaStream_t stream) {
+    const int n_tiles = (s.T + kBlockK - 1) / kBlockK, BH = s.B * H;
+    const int chunk = heads_per_chunk(BH, n_tiles, s.T, D, num_sms);
+    const dim3 grid(static_cast<unsigned>(n_tiles) * BH);  // one CTA per item; those that do not start are taken over
+    auto go = [&](auto kernel) {
+        return launch_overlapped(kernel, grid, dim3(kThreads), kSmemBytes, stream, tmQ, tmK, tmV, tmdO, tmdK, tmdV, LSE, Delta,
+                                 s.T, BH, H, orders, n_tiles, chunk, s.scale, dev_status, win != nullptr ? *win : Window{});
+    };
+    if (win != nullptr) return strided ? go(attn_dkdv_kernel<true, true, true>) : go(attn_dkdv_kernel<true, false, true>);
+    if (s.causal) return strided ? go(attn_dkdv_kernel<true, true, false>) : go(attn_dkdv_kernel<true, false, false>);
+    return strided ? go(attn_dkdv_kernel<false, true, false>) : go(attn_dkdv_kernel<false, false, false>);
+}
+}  // namespace
 
 cudaError_t launch_attn_dkdv(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
                              const CUtensorMap& tmdO, const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided,
                              uint32_t orders, const float* LSE, const float* Delta, const AttnShape& s, int num_sms,
                              int* dev_status, cudaStream_t stream) {
-    const int n_tiles = (s.T + kBlockK - 1) / kBlockK, BH = s.B * s.H;
-    const int chunk = heads_per_chunk(BH, n_tiles, s.T, D, num_sms);
-    const dim3 grid(static_cast<unsigned>(n_tiles) * BH);  // one CTA per item; those that do not start are taken over
-    auto go = [&](auto kernel) {
-        return launch_overlapped(kernel, grid, dim3(kThreads), kSmemBytes, stream, tmQ, tmK, tmV, tmdO, tmdK, tmdV, LSE, Delta,
-                                 s.T, BH, s.H, orders, n_tiles, chunk, s.scale, dev_status);
-    };
-    if (s.causal) return strided ? go(attn_dkdv_kernel<true, true>) : go(attn_dkdv_kernel<true, false>);
-    return strided ? go(attn_dkdv_kernel<false, true>) : go(attn_dkdv_kernel<false, false>);
+    return launch_dkdv(tmQ, tmK, tmV, tmdO, tmdK, tmdV, strided, orders, LSE, Delta, s, s.H, nullptr, num_sms, dev_status, stream);
+}
+
+cudaError_t launch_window_dkdv(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
+                               const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided, uint32_t orders, const float* LSE,
+                               const float* Delta, const AttnShape& s, const Window& win, int num_sms, int* dev_status,
+                               cudaStream_t stream) {
+    return launch_dkdv(tmQ, tmK, tmV, tmdO, tmdK, tmdV, strided, orders, LSE, Delta, s, s.H / win.group, &win, num_sms, dev_status,
+                       stream);
 }
 
 }  // namespace nova

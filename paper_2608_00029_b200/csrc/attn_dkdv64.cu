@@ -75,17 +75,24 @@ struct Kv64Bars {
 };
 static_assert(sizeof(Kv64Bars) <= 512, "barrier block");
 
-// Work items: 128-key tiles, heaviest (first) tiles first.
+// Work items: 128-key tiles, heaviest (first) tiles first.  kWindow: the heads are those of K and V, and an item has the steps of
+// all query heads that share its head, one after another.
+template <bool kWindow>
 struct Kv64Work {
     int BH, T, H;
     uint32_t orders;  // coordinate orders of the Q, K, V, dO, dK, dV tensor maps, four bits each
     bool causal;
+    Window win;
+    // Steps of one query head in an item of n.
+    __device__ __forceinline__ int per_head(int kt, int n) const {
+        return kWindow ? query_steps(win, kt * kBlockK, kBlockK, T, kStep) : n;
+    }
     // Key tile, head, first step and number of steps of item `idx`.
     __device__ __forceinline__ void get(int idx, int* kt, int* bh, int* s0, int* n) const {
         *kt = idx / BH;
         *bh = idx - *kt * BH;
         *s0 = causal ? *kt * (kBlockK / kStep) : 0;
-        *n = (T + kStep - 1) / kStep - *s0;
+        *n = kWindow ? win.group * query_steps(win, *kt * kBlockK, kBlockK, T, kStep) : (T + kStep - 1) / kStep - *s0;
     }
 };
 
@@ -131,10 +138,10 @@ __global__ void __launch_bounds__(256) row_terms64_kernel(const float* __restric
     *reinterpret_cast<uint4*>(row + kExtCore) = t.second;
 }
 
-template <bool kStrided, bool kTerms>
+template <bool kStrided, bool kTerms, bool kWindow>
 __device__ __forceinline__ void kv64_producer(const CUtensorMap* tmQ, const CUtensorMap* tmK, const CUtensorMap* tmV,
                                               const CUtensorMap* tmdO, const uint8_t* __restrict__ terms, uint8_t* smem,
-                                              Kv64Bars* bars, const Kv64Work& wk) {
+                                              Kv64Bars* bars, const Kv64Work<kWindow>& wk) {
     volatile int* abort_flag = &bars->abort_flag;
     bool ok = true;
     int w = 0, n_kv = 0, n_clc = 0, g = 0, st = 0;  // items; K and V, answers, steps requested
@@ -155,6 +162,8 @@ __device__ __forceinline__ void kv64_producer(const CUtensorMap* tmQ, const CUte
                                 kt * kBlockK, head, batch, bh);
         tma_load_tile<kStrided>(smem + kOffV + ks * kTileBytes, tmV, &bars->kv_full[ks], (wk.orders >> 8) & 15, 0,
                                 kt * kBlockK, head, batch, bh);
+        const int per = wk.per_head(kt, n);
+        int q_head = kWindow ? head * wk.win.group : head, q_bh = kWindow ? bh * wk.win.group : bh, sh = 0;
         for (int s = 0; s < n; ++s) {
             ok = mbar_wait(&bars->q_empty[st], ph ^ 1, abort_flag);
             if (!ok) break;
@@ -162,12 +171,17 @@ __device__ __forceinline__ void kv64_producer(const CUtensorMap* tmQ, const CUte
             ++g;
             if (kTerms)
                 bulk_load(smem + kOffExt + st * kExtStep,
-                          terms + (static_cast<size_t>(bh) * ((wk.T + kStep - 1) / kStep) + s0 + s) * kExtStep, kExtStep,
+                          terms + (static_cast<size_t>(q_bh) * ((wk.T + kStep - 1) / kStep) + s0 + sh) * kExtStep, kExtStep,
                           &bars->q_full[st]);
             tma_load_tile<kStrided>(smem + kOffQ + st * kStepBytes, tmQ, &bars->q_full[st], wk.orders & 15, 0,
-                                    (s0 + s) * kStep, head, batch, bh);
+                                    (s0 + sh) * kStep, q_head, batch, q_bh);
             tma_load_tile<kStrided>(smem + kOffdO + st * kStepBytes, tmdO, &bars->q_full[st], (wk.orders >> 12) & 15, 0,
-                                    (s0 + s) * kStep, head, batch, bh);
+                                    (s0 + sh) * kStep, q_head, batch, q_bh);
+            if (++sh == per) {  // on to the next query head
+                sh = 0;
+                ++q_head;
+                ++q_bh;
+            }
             if (++st == kQStages) {
                 st = 0;
                 ph ^= 1;
@@ -320,8 +334,9 @@ __device__ __forceinline__ void kv64_mma_acc(uint8_t* smem, Kv64Bars* bars, uint
 }
 
 // Compute group `grp` (steps g with g % 2 == grp), warp `cwarp` of it.
-template <bool kCausal>
-__device__ __forceinline__ void kv64_compute(Kv64Bars* bars, uint32_t tmem_base, float scale, int grp, int cwarp, int lane) {
+template <bool kCausal, bool kWindow>
+__device__ __forceinline__ void kv64_compute(Kv64Bars* bars, uint32_t tmem_base, float scale, const Kv64Work<kWindow>& wk, int grp,
+                                             int cwarp, int lane) {
     volatile int* abort_flag = &bars->abort_flag;
     const uint32_t lane_base = 32u * cwarp;
     const int r = lane_base + lane;  // local key row
@@ -334,12 +349,17 @@ __device__ __forceinline__ void kv64_compute(Kv64Bars* bars, uint32_t tmem_base,
     uint32_t ph = 0;   // phase of this group's barriers
 
     for (int w = 0;; ++w) {
-        const int n = bars->ring.take_steps(w, lane, abort_flag);
+        int item = 0;
+        const int n = bars->ring.take_steps(w, lane, abort_flag, kWindow ? &item : nullptr);
         if (n <= 0) {
             ok = (n == 0);
             break;
         }
-        for (int s = (g ^ grp) & 1; s < n; s += 2, ph ^= 1) {
+        const int kt = kWindow ? item / wk.BH : 0, per = wk.per_head(kt, n);
+        int sh = (g ^ grp) & 1;  // the step in its query head
+        for (int s = (g ^ grp) & 1; s < n; s += 2, sh += 2, ph ^= 1) {
+            if constexpr (kWindow)
+                while (sh >= per) sh -= per;
             ok = mbar_wait(&bars->s_full[grp], ph, abort_flag);
             if (!ok) break;
             tc_fence_after();
@@ -361,7 +381,15 @@ __device__ __forceinline__ void kv64_compute(Kv64Bars* bars, uint32_t tmem_base,
             // Keep key <= query (the first steps of a causal item).  Keys past the end of the sequence need no mask: their
             // rows are not stored.
             const int first = r - s * kStep;  // first kept query of the step
-            if (kCausal && s < kBlockK / kStep) {
+            if constexpr (kWindow) {
+                const int q0 = kt * kBlockK + sh * kStep;
+                if (any_dropping(wk.win, kt * kBlockK, q0)) {
+                    const uint64_t kept = keeping_queries(wk.win, kt * kBlockK + r, q0);
+#pragma unroll
+                    for (int i = 0; i < kStep; ++i)
+                        if (!(static_cast<uint32_t>(kept >> (i & 32)) >> (i & 31) & 1u)) pf[i] = 0u;
+                }
+            } else if (kCausal && s < kBlockK / kStep) {
 #pragma unroll
                 for (int i = 0; i < kStep; ++i)
                     if (i < first) pf[i] = 0u;
@@ -412,10 +440,11 @@ __device__ __forceinline__ void kv64_compute(Kv64Bars* bars, uint32_t tmem_base,
 //   dV and dK * scale of a finished item as bf16 into shared memory and out with TMA stores.
 // The stages of an item's first kQStages steps are handed back by the item before, whose dV and dK may wait till then; the
 // later ones only after dV and dK have been read out.
-template <bool kStrided, bool kTerms>
+template <bool kStrided, bool kTerms, bool kWindow>
 __device__ __forceinline__ void kv64_edges(uint8_t* smem, Kv64Bars* bars, uint32_t tmem_base, const CUtensorMap* tmdK,
                                            const CUtensorMap* tmdV, const float* __restrict__ LSE,
-                                           const float* __restrict__ Delta, float scale, const Kv64Work& wk, int ow, int lane) {
+                                           const float* __restrict__ Delta, float scale, const Kv64Work<kWindow>& wk, int ow,
+                                           int lane) {
     volatile int* abort_flag = &bars->abort_flag;
     const uint32_t lane_base = 32u * ow;
     const int r = lane_base + lane;
@@ -555,18 +584,19 @@ __device__ __forceinline__ void kv64_edges(uint8_t* smem, Kv64Bars* bars, uint32
     if (leader) bulk_wait_group<0>();  // dV and dK must be complete before the kernel ends
 }
 
-template <bool kCausal, bool kStrided, bool kTerms>
+template <bool kCausal, bool kStrided, bool kTerms, bool kWindow>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_dkdv64_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                    const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmdO,
                    const __grid_constant__ CUtensorMap tmdK, const __grid_constant__ CUtensorMap tmdV,
                    const float* __restrict__ LSE, const float* __restrict__ Delta, const uint8_t* __restrict__ terms, int T, int BH,
-                   int H, uint32_t orders, float scale, int* __restrict__ dev_status) {
+                   int H, uint32_t orders, float scale, int* __restrict__ dev_status, const Window win) {
+    static_assert(!kWindow || (kCausal && kTerms), "with the window the row terms are prepared");
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     Kv64Bars* bars = reinterpret_cast<Kv64Bars*>(smem + kOffBar);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Kv64Work wk{BH, T, H, orders, kCausal};
+    const Kv64Work<kWindow> wk{BH, T, H, orders, kCausal, win};
 
     // The kernel before this one in the stream is the dQ kernel, of which nothing is needed: it need not have completed (ptx.cuh).
     // The threads that will read global memory, the producer and the edge warps, see to it while the others set up.
@@ -626,7 +656,7 @@ attn_dkdv64_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     griddep_launch_dependents();
 
     if (warp == 0) {
-        if (lane == 0) kv64_producer<kStrided, kTerms>(&tmQ, &tmK, &tmV, &tmdO, terms, smem, bars, wk);
+        if (lane == 0) kv64_producer<kStrided, kTerms, kWindow>(&tmQ, &tmK, &tmV, &tmdO, terms, smem, bars, wk);
     } else if (warp == 1) {
         kv64_mma_sp<false>(smem, bars, tmem_base);
     } else if (warp == 2) {
@@ -634,9 +664,9 @@ attn_dkdv64_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     } else if (warp == 3) {
         kv64_mma_acc(smem, bars, tmem_base);
     } else if (warp >= 12) {
-        kv64_edges<kStrided, kTerms>(smem, bars, tmem_base, &tmdK, &tmdV, LSE, Delta, scale, wk, warp & 3, lane);
+        kv64_edges<kStrided, kTerms, kWindow>(smem, bars, tmem_base, &tmdK, &tmdV, LSE, Delta, scale, wk, warp & 3, lane);
     } else {
-        kv64_compute<kCausal>(bars, tmem_base, scale, (warp - 4) >> 2, warp & 3, lane);
+        kv64_compute<kCausal, kWindow>(bars, tmem_base, scale, wk, (warp - 4) >> 2, warp & 3, lane);
     }
 
     tc_fence_before();
@@ -653,12 +683,14 @@ cudaError_t configure_attn_dkdv64() {
     auto set = [](auto kernel) {
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
     };
-    cudaError_t e = set(attn_dkdv64_kernel<true, false, false>);
-    if (e == cudaSuccess) e = set(attn_dkdv64_kernel<false, false, false>);
-    if (e == cudaSuccess) e = set(attn_dkdv64_kernel<true, false, true>);
-    if (e == cudaSuccess) e = set(attn_dkdv64_kernel<true, true, true>);
-    if (e == cudaSuccess) e = set(attn_dkdv64_kernel<false, false, true>);
-    if (e == cudaSuccess) e = set(attn_dkdv64_kernel<false, true, true>);
+    cudaError_t e = set(attn_dkdv64_kernel<true, false, false, false>);
+    if (e == cudaSuccess) e = set(attn_dkdv64_kernel<false, false, false, false>);
+    if (e == cudaSuccess) e = set(attn_dkdv64_kernel<true, false, true, false>);
+    if (e == cudaSuccess) e = set(attn_dkdv64_kernel<true, true, true, false>);
+    if (e == cudaSuccess) e = set(attn_dkdv64_kernel<false, false, true, false>);
+    if (e == cudaSuccess) e = set(attn_dkdv64_kernel<false, true, true, false>);
+    if (e == cudaSuccess) e = set(attn_dkdv64_kernel<true, false, true, true>);
+    if (e == cudaSuccess) e = set(attn_dkdv64_kernel<true, true, true, true>);
     return e;
 }
 
@@ -669,20 +701,41 @@ cudaError_t launch_row_terms64(const float* LSE, const float* Delta, void* terms
                              static_cast<uint8_t*>(terms), s.T, n_steps, rows, 1.0f / fmaxf(s.scale, kLeastScale));
 }
 
+namespace {
+// H: heads of K and V in a sequence.
+cudaError_t launch_dkdv64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
+                          const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided, uint32_t orders, const float* LSE,
+                          const float* Delta, const void* terms, const AttnShape& s, int H, const Window* win, int* dev_status,
+                          cudaStream_t stream) {
+    if ((strided || win != nullptr) && terms == nullptr) return cudaErrorNotSupported;  // (only the deterministic entry point has no workspace)
+    const int n_tiles = (s.T + kBlockK - 1) / kBlockK, BH = s.B * H;
+    const dim3 grid(static_cast<unsigned>(n_tiles) * BH);  // one CTA per item; those that do not start are taken over
+    auto go = [&](auto kernel) {
+        return launch_overlapped(kernel, grid, dim3(kThreads), kSmemBytes, stream, tmQ, tmK, tmV, tmdO, tmdK, tmdV, LSE, Delta,
+                                 static_cast<const uint8_t*>(terms), s.T, BH, H, orders, s.scale, dev_status,
+                                 win != nullptr ? *win : Window{});
+    };
+    if (win != nullptr) return strided ? go(attn_dkdv64_kernel<true, true, true, true>) : go(attn_dkdv64_kernel<true, false, true, true>);
+    if (terms == nullptr)
+        return s.causal ? go(attn_dkdv64_kernel<true, false, false, false>) : go(attn_dkdv64_kernel<false, false, false, false>);
+    if (s.causal) return strided ? go(attn_dkdv64_kernel<true, true, true, false>) : go(attn_dkdv64_kernel<true, false, true, false>);
+    return strided ? go(attn_dkdv64_kernel<false, true, true, false>) : go(attn_dkdv64_kernel<false, false, true, false>);
+}
+}  // namespace
+
 cudaError_t launch_attn_dkdv64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
                                const CUtensorMap& tmdO, const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided,
                                uint32_t orders, const float* LSE, const float* Delta, const void* terms, const AttnShape& s,
                                int* dev_status, cudaStream_t stream) {
-    if (strided && terms == nullptr) return cudaErrorNotSupported;  // (only the deterministic entry point has no workspace)
-    const int n_tiles = (s.T + kBlockK - 1) / kBlockK, BH = s.B * s.H;
-    const dim3 grid(static_cast<unsigned>(n_tiles) * BH);  // one CTA per item; those that do not start are taken over
-    auto go = [&](auto kernel) {
-        return launch_overlapped(kernel, grid, dim3(kThreads), kSmemBytes, stream, tmQ, tmK, tmV, tmdO, tmdK, tmdV, LSE, Delta,
-                                 static_cast<const uint8_t*>(terms), s.T, BH, s.H, orders, s.scale, dev_status);
-    };
-    if (terms == nullptr) return s.causal ? go(attn_dkdv64_kernel<true, false, false>) : go(attn_dkdv64_kernel<false, false, false>);
-    if (s.causal) return strided ? go(attn_dkdv64_kernel<true, true, true>) : go(attn_dkdv64_kernel<true, false, true>);
-    return strided ? go(attn_dkdv64_kernel<false, true, true>) : go(attn_dkdv64_kernel<false, false, true>);
+    return launch_dkdv64(tmQ, tmK, tmV, tmdO, tmdK, tmdV, strided, orders, LSE, Delta, terms, s, s.H, nullptr, dev_status, stream);
+}
+
+cudaError_t launch_window_dkdv64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
+                                 const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided, uint32_t orders, const float* LSE,
+                                 const float* Delta, const void* terms, const AttnShape& s, const Window& win, int* dev_status,
+                                 cudaStream_t stream) {
+    return launch_dkdv64(tmQ, tmK, tmV, tmdO, tmdK, tmdV, strided, orders, LSE, Delta, terms, s, s.H / win.group, &win, dev_status,
+                         stream);
 }
 
 }  // namespace nova

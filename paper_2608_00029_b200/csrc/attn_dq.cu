@@ -82,11 +82,13 @@ static_assert(sizeof(DqBars) <= 512, "barrier block");
 // chunks of heads whose tensors stay in L2 together (the exact Delta at B=16, H=32, T=1024 175 -> 157 us, the
 // deterministic backward 650 -> 627 us); at D=64 a head's K and V are half as large and the longer arithmetic costs
 // 1 % where there is nothing to gain.
-template <int D, int kTiles>
+template <int D, int kTiles, bool kWindow>
 struct DqWork {
     int BH, n_blocks, chunk, T, H;
     uint32_t orders;  // coordinate orders of the Q, K, V, dO, dQ tensor maps, four bits each
     bool causal;
+    Window win;  // kWindow: single tiles only
+    __device__ __forceinline__ KeySpan span(int blk) const { return key_span(win, blk * kBlockQ, kBlockQ, T, kStep); }
     // Block index, head, and the number of key steps each tile visits (0: the tile lies past the end of the sequence).
     __device__ __forceinline__ void get(int idx, int* blk, int* bh, int* n_a, int* n_b) const {
         if constexpr (D == 128) {
@@ -104,6 +106,11 @@ struct DqWork {
             *blk = n_blocks - 1 - idx / BH;
             *bh = idx % BH;
         }
+        if constexpr (kWindow) {
+            *n_a = span(*blk).n;
+            *n_b = 0;
+            return;
+        }
         const int n_all = (T + kStep - 1) / kStep;
         const int qt_a = kTiles * (*blk), qt_b = qt_a + 1;
         *n_a = causal ? min((qt_a + 1) * (kBlockQ / kStep), n_all) : n_all;
@@ -111,9 +118,10 @@ struct DqWork {
     }
 };
 
-template <int D, int kTiles, bool kStrided>
+template <int D, int kTiles, bool kStrided, bool kWindow>
 __device__ __forceinline__ void dq_producer(const CUtensorMap* tmQ, const CUtensorMap* tmK, const CUtensorMap* tmV,
-                                            const CUtensorMap* tmdO, uint8_t* smem, DqBars* bars, const DqWork<D, kTiles>& wk) {
+                                            const CUtensorMap* tmdO, uint8_t* smem, DqBars* bars,
+                                            const DqWork<D, kTiles, kWindow>& wk) {
     using Cfg = DqCfg<D, kTiles>;
     volatile int* abort_flag = &bars->abort_flag;
     constexpr long long limit = kWaitLimitCycles;
@@ -129,6 +137,9 @@ __device__ __forceinline__ void dq_producer(const CUtensorMap* tmQ, const CUtens
         int blk, bh, n_a, n_b;
         wk.get(item, &blk, &bh, &n_a, &n_b);
         const int head = kStrided ? bh % wk.H : 0, batch = kStrided ? bh / wk.H : 0;
+        // with the window: the key/value head that the query head shares, and the steps in its reach
+        const int kv_head = kWindow ? head / wk.win.group : head, kv_bh = kWindow ? bh / wk.win.group : bh;
+        const KeySpan span = kWindow ? wk.span(blk) : KeySpan{0, 0, 0};
         const int qs = w % Cfg::kQStages;
         const uint32_t qph = (w / Cfg::kQStages) & 1;
         const int n = max(n_a, n_b);
@@ -154,12 +165,13 @@ __device__ __forceinline__ void dq_producer(const CUtensorMap* tmQ, const CUtens
             if (!ok) break;
             mbar_expect_tx(&bars->kv_full[st], 2 * Cfg::kStepBytes);
             armed_kv[st] = ph;
+            const int key0 = (kWindow ? span.at(j) : j) * kStep;
 #pragma unroll
             for (int h = 0; h < Cfg::kHalves; ++h) {
                 tma_load_tile<kStrided>(smem + Cfg::kOffK + st * Cfg::kStepBytes + h * kHalfStepBytes, tmK,
-                                        &bars->kv_full[st], (wk.orders >> 4) & 15, h * kBoxCols, j * kStep, head, batch, bh);
+                                        &bars->kv_full[st], (wk.orders >> 4) & 15, h * kBoxCols, key0, kv_head, batch, kv_bh);
                 tma_load_tile<kStrided>(smem + Cfg::kOffV + st * Cfg::kStepBytes + h * kHalfStepBytes, tmV,
-                                        &bars->kv_full[st], (wk.orders >> 8) & 15, h * kBoxCols, j * kStep, head, batch, bh);
+                                        &bars->kv_full[st], (wk.orders >> 8) & 15, h * kBoxCols, key0, kv_head, batch, kv_bh);
             }
             if (++st == Cfg::kKVStages) {
                 st = 0;
@@ -191,8 +203,8 @@ __device__ __forceinline__ void dq_producer(const CUtensorMap* tmQ, const CUtens
 }
 
 // The issuer of query tile t: the whole warp in uniform control flow, one elected lane issues.
-template <int D, int kTiles, bool kDelta>
-__device__ __forceinline__ void dq_mma(uint8_t* smem, DqBars* bars, uint32_t tmem_base, const DqWork<D, kTiles>& wk, int t) {
+template <int D, int kTiles, bool kDelta, bool kWindow>
+__device__ __forceinline__ void dq_mma(uint8_t* smem, DqBars* bars, uint32_t tmem_base, const DqWork<D, kTiles, kWindow>& wk, int t) {
     using Cfg = DqCfg<D, kTiles>;
     volatile int* abort_flag = &bars->abort_flag;
     constexpr uint32_t kIdescT = umma_idesc_bf16(128, kStep, 0, 0);  // S, dP
@@ -345,11 +357,11 @@ __device__ __forceinline__ void dq_mma(uint8_t* smem, DqBars* bars, uint32_t tme
 }
 
 // The row warps of query tile t.
-template <int D, int kTiles, bool kCausal, bool kStrided, bool kDelta>
+template <int D, int kTiles, bool kCausal, bool kStrided, bool kDelta, bool kWindow>
 __device__ __forceinline__ void dq_rows(uint8_t* smem, DqBars* bars, uint32_t tmem_base, const CUtensorMap* tmdQ,
                                         const float* __restrict__ LSE, const float* __restrict__ Delta,
-                                        float* __restrict__ Delta_out, float scale, const DqWork<D, kTiles>& wk, int t, int rwarp,
-                                        int lane) {
+                                        float* __restrict__ Delta_out, float scale, const DqWork<D, kTiles, kWindow>& wk, int t,
+                                        int rwarp, int lane) {
     using Cfg = DqCfg<D, kTiles>;
     volatile int* abort_flag = &bars->abort_flag;
     const uint32_t lane_base = 32u * rwarp;
@@ -375,6 +387,7 @@ __device__ __forceinline__ void dq_rows(uint8_t* smem, DqBars* bars, uint32_t tm
         const int qt = kTiles * blk + t;
         const int row = qt * kBlockQ + row_local;
         const size_t idx = static_cast<size_t>(bh) * T + row;
+        const KeySpan span = kWindow ? wk.span(blk) : KeySpan{0, 0, 0};
         const int qs = w % Cfg::kQStages;
         if (n_t == 0) {  // tile past the end of the sequence: only release its buffers, once they have been filled
             bool leader_ok = true;
@@ -419,11 +432,21 @@ __device__ __forceinline__ void dq_rows(uint8_t* smem, DqBars* bars, uint32_t tm
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars->sp_free[buf][t]);
             // Mask from indices only: causal keeps key <= query, the end of the sequence key < T.
-            const int lim = (kCausal ? min(row, T - 1) : T - 1) - j * kStep;  // last kept key of the step
-            if ((kCausal && (j + 1) * kStep > qt * kBlockQ) || (j + 1) * kStep > T) {
+            if constexpr (kWindow) {  // (rows past the end of the sequence keep what the last one does, and have no weight)
+                const int key0 = span.at(j) * kStep, last = min(qt * kBlockQ + kBlockQ, T) - 1;
+                if (any_dropped(wk.win, qt * kBlockQ, last, key0)) {
+                    const uint64_t kept = kept_keys(wk.win, min(row, T - 1), key0);
 #pragma unroll
-                for (int i = 0; i < kStep; ++i)
-                    if (i > lim) sv[i] = 0xff800000u;  // -inf: P = 0
+                    for (int i = 0; i < kStep; ++i)
+                        if (!(static_cast<uint32_t>(kept >> (i & 32)) >> (i & 31) & 1u)) sv[i] = 0xff800000u;  // -inf: P = 0
+                }
+            } else {
+                const int lim = (kCausal ? min(row, T - 1) : T - 1) - j * kStep;  // last kept key of the step
+                if ((kCausal && (j + 1) * kStep > qt * kBlockQ) || (j + 1) * kStep > T) {
+#pragma unroll
+                    for (int i = 0; i < kStep; ++i)
+                        if (i > lim) sv[i] = 0xff800000u;  // -inf: P = 0
+                }
             }
             uint32_t ds[kStep / 2];
 #pragma unroll
@@ -537,11 +560,11 @@ __device__ __forceinline__ void dq_rows(uint8_t* smem, DqBars* bars, uint32_t tm
 }
 
 // Set-up and roles, shared by the two builds below.
-template <int D, int kTiles, bool kCausal, bool kStrided, bool kDelta>
+template <int D, int kTiles, bool kCausal, bool kStrided, bool kDelta, bool kWindow>
 __device__ __forceinline__ void dq_body(const CUtensorMap* tmQ, const CUtensorMap* tmK, const CUtensorMap* tmV,
                                         const CUtensorMap* tmdO, const CUtensorMap* tmdQ, const float* __restrict__ LSE,
-                                        const float* __restrict__ Delta, float* __restrict__ Delta_out, const DqWork<D, kTiles>& wk,
-                                        float scale, int* __restrict__ dev_status) {
+                                        const float* __restrict__ Delta, float* __restrict__ Delta_out,
+                                        const DqWork<D, kTiles, kWindow>& wk, float scale, int* __restrict__ dev_status) {
     using Cfg = DqCfg<D, kTiles>;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -587,12 +610,12 @@ __device__ __forceinline__ void dq_body(const CUtensorMap* tmQ, const CUtensorMa
     griddep_wait();  // everything above overlaps the previous kernel of the stream
 
     if (warp == 0) {
-        if (lane == 0) dq_producer<D, kTiles, kStrided>(tmQ, tmK, tmV, tmdO, smem, bars, wk);
+        if (lane == 0) dq_producer<D, kTiles, kStrided, kWindow>(tmQ, tmK, tmV, tmdO, smem, bars, wk);
     } else if (warp == 1 || (kTiles == 2 && warp == 3)) {
-        dq_mma<D, kTiles, kDelta>(smem, bars, tmem_base, wk, warp >> 1);
+        dq_mma<D, kTiles, kDelta, kWindow>(smem, bars, tmem_base, wk, warp >> 1);
     } else if (warp >= 4 && warp < 4 + 4 * kTiles) {
-        dq_rows<D, kTiles, kCausal, kStrided, kDelta>(smem, bars, tmem_base, tmdQ, LSE, Delta, Delta_out, scale, wk,
-                                                      (warp - 4) >> 2, warp & 3, lane);
+        dq_rows<D, kTiles, kCausal, kStrided, kDelta, kWindow>(smem, bars, tmem_base, tmdQ, LSE, Delta, Delta_out, scale, wk,
+                                                               (warp - 4) >> 2, warp & 3, lane);
     }
 
     tc_fence_before();
@@ -601,14 +624,16 @@ __device__ __forceinline__ void dq_body(const CUtensorMap* tmQ, const CUtensorMa
     if (threadIdx.x == 0 && bars->abort_flag != 0) atomicExch(dev_status, kDevTimeout);
 }
 
-template <int D, int kTiles, bool kCausal, bool kStrided>
+template <int D, int kTiles, bool kCausal, bool kStrided, bool kWindow>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_dq_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmdO,
                const __grid_constant__ CUtensorMap tmdQ, const float* __restrict__ LSE, const float* __restrict__ Delta,
-               int T, int BH, int H, uint32_t orders, int n_blocks, int chunk, float scale, int* __restrict__ dev_status) {
+               int T, int BH, int H, uint32_t orders, int n_blocks, int chunk, float scale, int* __restrict__ dev_status,
+               const Window win) {
     dq_body<D, kTiles, kCausal, kStrided, false>(&tmQ, &tmK, &tmV, &tmdO, &tmdQ, LSE, Delta, nullptr,
-                                                 DqWork<D, kTiles>{BH, n_blocks, chunk, T, H, orders, kCausal}, scale, dev_status);
+                                                 DqWork<D, kTiles, kWindow>{BH, n_blocks, chunk, T, H, orders, kCausal, win}, scale,
+                                                 dev_status);
 }
 
 template <int D, int kTiles, bool kCausal>
@@ -618,7 +643,8 @@ attn_delta_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                   const float* __restrict__ LSE, float* __restrict__ Delta, int T, int BH, int n_blocks, int chunk, float scale,
                   int* __restrict__ dev_status) {
     dq_body<D, kTiles, kCausal, false, true>(&tmQ, &tmK, &tmV, &tmdO, nullptr, LSE, nullptr, Delta,
-                                             DqWork<D, kTiles>{BH, n_blocks, chunk, T, 1, 0u, kCausal}, scale, dev_status);
+                                             DqWork<D, kTiles, false>{BH, n_blocks, chunk, T, 1, 0u, kCausal, Window{}}, scale,
+                                             dev_status);
 }
 
 // Key steps after which the last SM is done.  Every item costs two besides its own.
@@ -678,8 +704,12 @@ cudaError_t configure_attn_dq() {
             };
             cudaError_t r = set(attn_delta_kernel<D, kTiles, kCausal>);
             if constexpr (D == 128) {
-                if (r == cudaSuccess) r = set(attn_dq_kernel<D, kTiles, kCausal, false>);
-                if (r == cudaSuccess) r = set(attn_dq_kernel<D, kTiles, kCausal, true>);
+                if (r == cudaSuccess) r = set(attn_dq_kernel<D, kTiles, kCausal, false, false>);
+                if (r == cudaSuccess) r = set(attn_dq_kernel<D, kTiles, kCausal, true, false>);
+                if constexpr (kTiles == 1 && kCausal) {
+                    if (r == cudaSuccess) r = set(attn_dq_kernel<D, 1, true, false, true>);
+                    if (r == cudaSuccess) r = set(attn_dq_kernel<D, 1, true, true, true>);
+                }
             }
             return r;
         });
@@ -700,11 +730,24 @@ cudaError_t launch_attn_dq(const CUtensorMap& tmQ, const CUtensorMap& tmK, const
             auto go = [&](auto kernel) {
                 return launch_overlapped(kernel, p.grid, dim3(kThreads), DqCfg<D, kTiles>::kSmemBytes, stream, tmQ, tmK, tmV,
                                          tmdO, tmdQ, LSE, Delta, s.T, s.B * s.H, s.H, orders, p.n_blocks, p.chunk, s.scale,
-                                         dev_status);
+                                         dev_status, Window{});
             };
-            return strided ? go(attn_dq_kernel<D, kTiles, kCausal, true>) : go(attn_dq_kernel<D, kTiles, kCausal, false>);
+            return strided ? go(attn_dq_kernel<D, kTiles, kCausal, true, false>) : go(attn_dq_kernel<D, kTiles, kCausal, false, false>);
         }
     });
+}
+
+cudaError_t launch_window_dq(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
+                             const CUtensorMap& tmdQ, bool strided, uint32_t orders, const float* LSE, const float* Delta,
+                             const AttnShape& s, const Window& win, int num_sms, int* dev_status, cudaStream_t stream) {
+    const int n_blocks = (s.T + kBlockQ - 1) / kBlockQ, BH = s.B * s.H;
+    const int chunk = heads_per_chunk(BH, n_blocks, s.T, s.D, num_sms);
+    const dim3 grid(static_cast<unsigned>(n_blocks) * BH);
+    auto go = [&](auto kernel) {
+        return launch_overlapped(kernel, grid, dim3(kThreads), DqCfg<128, 1>::kSmemBytes, stream, tmQ, tmK, tmV, tmdO, tmdQ, LSE,
+                                 Delta, s.T, BH, s.H, orders, n_blocks, chunk, s.scale, dev_status, win);
+    };
+    return strided ? go(attn_dq_kernel<128, 1, true, true, true>) : go(attn_dq_kernel<128, 1, true, false, true>);
 }
 
 cudaError_t launch_attn_delta(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,

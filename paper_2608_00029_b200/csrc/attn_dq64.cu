@@ -64,23 +64,30 @@ struct Dq64Bars {
 static_assert(sizeof(Dq64Bars) <= 512, "barrier block");
 
 // Work items: 128-row query tiles, heaviest first (the last tile of a causal problem sees every key).
+template <bool kWindow>
 struct Dq64Work {
     int BH, n_tiles, T, H;
     uint32_t orders;  // coordinate orders of the Q, K, V, dO, dQ tensor maps, four bits each
     bool causal;
+    Window win;
+    __device__ __forceinline__ KeySpan span(int qt) const { return key_span(win, qt * kBlockQ, kBlockQ, T, kStep); }
     // Query tile, head and number of key steps of item `idx`.
     __device__ __forceinline__ void get(int idx, int* qt, int* bh, int* n) const {
         const int order = idx / BH;
         *qt = n_tiles - 1 - order;
         *bh = idx - order * BH;
+        if constexpr (kWindow) {
+            *n = span(*qt).n;
+            return;
+        }
         const int n_all = (T + kStep - 1) / kStep;
         *n = causal ? min((*qt + 1) * (kBlockQ / kStep), n_all) : n_all;
     }
 };
 
-template <bool kStrided>
+template <bool kStrided, bool kWindow>
 __device__ __forceinline__ void dq64_producer(const CUtensorMap* tmQ, const CUtensorMap* tmK, const CUtensorMap* tmV,
-                                              const CUtensorMap* tmdO, uint8_t* smem, Dq64Bars* bars, const Dq64Work& wk) {
+                                              const CUtensorMap* tmdO, uint8_t* smem, Dq64Bars* bars, const Dq64Work<kWindow>& wk) {
     volatile int* abort_flag = &bars->abort_flag;
     bool ok = true, clc_pending = false;
     int w = 0, n_q = 0, g = 0, st = 0;  // items, Q and dO requested; steps requested
@@ -93,6 +100,9 @@ __device__ __forceinline__ void dq64_producer(const CUtensorMap* tmQ, const CUte
         wk.get(item, &qt, &bh, &n);
         if (w == 0) griddep_wait();
         const int head = kStrided ? bh % wk.H : 0, batch = kStrided ? bh / wk.H : 0;
+        // with the window: the key/value head that the query head shares, and the steps in its reach
+        const int kv_head = kWindow ? head / wk.win.group : head, kv_bh = kWindow ? bh / wk.win.group : bh;
+        const KeySpan span = kWindow ? wk.span(qt) : KeySpan{0, 0, 0};
         const int qs = w & 1;
         ok = mbar_wait(&bars->q_empty[qs], ((w >> 1) & 1) ^ 1, abort_flag);
         if (!ok) break;
@@ -107,10 +117,11 @@ __device__ __forceinline__ void dq64_producer(const CUtensorMap* tmQ, const CUte
             if (!ok) break;
             mbar_expect_tx(&bars->kv_full[st], 2 * kStepBytes);
             ++g;
-            tma_load_tile<kStrided>(smem + kOffK + st * kStepBytes, tmK, &bars->kv_full[st], (wk.orders >> 4) & 15, 0, s * kStep,
-                                    head, batch, bh);
-            tma_load_tile<kStrided>(smem + kOffV + st * kStepBytes, tmV, &bars->kv_full[st], (wk.orders >> 8) & 15, 0, s * kStep,
-                                    head, batch, bh);
+            const int key0 = (kWindow ? span.at(s) : s) * kStep;
+            tma_load_tile<kStrided>(smem + kOffK + st * kStepBytes, tmK, &bars->kv_full[st], (wk.orders >> 4) & 15, 0, key0,
+                                    kv_head, batch, kv_bh);
+            tma_load_tile<kStrided>(smem + kOffV + st * kStepBytes, tmV, &bars->kv_full[st], (wk.orders >> 8) & 15, 0, key0,
+                                    kv_head, batch, kv_bh);
             if (++st == kStages) {
                 st = 0;
                 ph ^= 1;
@@ -136,8 +147,8 @@ __device__ __forceinline__ void dq64_producer(const CUtensorMap* tmQ, const CUte
 
 // S (kdP false) and dP (kdP true) of each step, as soon as the compute group has read those of its last step.  dP waits for
 // dQ of the group's last but one step besides, so that a group that sees both finds its buffer of dS free.
-template <bool kdP, bool kDelta>
-__device__ __forceinline__ void dq64_mma_sp(uint8_t* smem, Dq64Bars* bars, uint32_t tmem_base, const Dq64Work& wk) {
+template <bool kdP, bool kDelta, bool kWindow>
+__device__ __forceinline__ void dq64_mma_sp(uint8_t* smem, Dq64Bars* bars, uint32_t tmem_base, const Dq64Work<kWindow>& wk) {
     volatile int* abort_flag = &bars->abort_flag;
     constexpr uint32_t kIdescT = umma_idesc_bf16(128, kStep, 0, 0);
     const uint32_t hi = umma_desc_hi_sw128(1024);
@@ -192,7 +203,8 @@ __device__ __forceinline__ void dq64_mma_sp(uint8_t* smem, Dq64Bars* bars, uint3
 }
 
 // dQ of each step, in key order.
-__device__ __forceinline__ void dq64_mma_dq(uint8_t* smem, Dq64Bars* bars, uint32_t tmem_base, const Dq64Work& wk) {
+template <bool kWindow>
+__device__ __forceinline__ void dq64_mma_dq(uint8_t* smem, Dq64Bars* bars, uint32_t tmem_base, const Dq64Work<kWindow>& wk) {
     volatile int* abort_flag = &bars->abort_flag;
     constexpr uint32_t kIdescdQ = umma_idesc_bf16(128, D, 0, 1);  // A from TMEM, B (K) MN-major
     const uint32_t hi = umma_desc_hi_sw128(1024);
@@ -246,9 +258,9 @@ __device__ __forceinline__ void dq64_mma_dq(uint8_t* smem, Dq64Bars* bars, uint3
 }
 
 // Compute group `grp` (steps g with g % 2 == grp), warp `cwarp` of it.
-template <bool kCausal, bool kDelta>
-__device__ __forceinline__ void dq64_compute(uint8_t* smem, Dq64Bars* bars, uint32_t tmem_base, float scale, const Dq64Work& wk,
-                                             int grp, int cwarp, int lane) {
+template <bool kCausal, bool kDelta, bool kWindow>
+__device__ __forceinline__ void dq64_compute(uint8_t* smem, Dq64Bars* bars, uint32_t tmem_base, float scale,
+                                             const Dq64Work<kWindow>& wk, int grp, int cwarp, int lane) {
     volatile int* abort_flag = &bars->abort_flag;
     const uint32_t lane_base = 32u * cwarp;
     const int r = lane_base + lane;  // local query row
@@ -274,6 +286,7 @@ __device__ __forceinline__ void dq64_compute(uint8_t* smem, Dq64Bars* bars, uint
         const float2 row_terms = reinterpret_cast<const float2*>(smem + kOffRow)[(w & 1) * kBlockQ + r];
         const uint64_t nlse = f32x2_pack(row_terms.x, row_terms.x), nd = f32x2_pack(row_terms.y, row_terms.y);
         const int row = qt * kBlockQ + r;
+        const KeySpan span = kWindow ? wk.span(qt) : KeySpan{0, 0, 0};
         uint64_t acc0 = 0, acc1 = 0;
         for (int s = (g ^ grp) & 1; s < n; s += 2, ++k) {
             ok = mbar_wait(&bars->sp_full[grp], k & 1, abort_flag);
@@ -287,11 +300,21 @@ __device__ __forceinline__ void dq64_compute(uint8_t* smem, Dq64Bars* bars, uint
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars->s_free[grp]);
             // Mask from indices only: causal keeps key <= query, the end of the sequence key < T.
-            const int lim = (kCausal ? min(row, wk.T - 1) : wk.T - 1) - s * kStep;  // last kept key of the step
-            if ((kCausal && (s + 1) * kStep > qt * kBlockQ) || (s + 1) * kStep > wk.T) {
+            if constexpr (kWindow) {  // (rows past the end of the sequence keep what the last one does, and have no weight)
+                const int key0 = span.at(s) * kStep, last = min(qt * kBlockQ + kBlockQ, wk.T) - 1;
+                if (any_dropped(wk.win, qt * kBlockQ, last, key0)) {
+                    const uint64_t kept = kept_keys(wk.win, min(row, wk.T - 1), key0);
 #pragma unroll
-                for (int i = 0; i < kStep; ++i)
-                    if (i > lim) pf[i] = 0xff800000u;  // -inf: P = 0
+                    for (int i = 0; i < kStep; ++i)
+                        if (!(static_cast<uint32_t>(kept >> (i & 32)) >> (i & 31) & 1u)) pf[i] = 0xff800000u;  // -inf: P = 0
+                }
+            } else {
+                const int lim = (kCausal ? min(row, wk.T - 1) : wk.T - 1) - s * kStep;  // last kept key of the step
+                if ((kCausal && (s + 1) * kStep > qt * kBlockQ) || (s + 1) * kStep > wk.T) {
+#pragma unroll
+                    for (int i = 0; i < kStep; ++i)
+                        if (i > lim) pf[i] = 0xff800000u;  // -inf: P = 0
+                }
             }
 #pragma unroll
             for (int i = 0; i < kStep; i += 2) {
@@ -352,10 +375,11 @@ __device__ __forceinline__ void dq64_compute(uint8_t* smem, Dq64Bars* bars, uint
 // Edge warps (warp `ow` of four, thread = query row): Q and dO of an item from shared into tensor memory, each as soon as the
 // last product that reads these columns is done, and the row terms; then dQ * scale of the item before as bf16 into
 // shared memory and out with a TMA store, or its Delta.
-template <bool kStrided, bool kDelta>
+template <bool kStrided, bool kDelta, bool kWindow>
 __device__ __forceinline__ void dq64_edges(uint8_t* smem, Dq64Bars* bars, uint32_t tmem_base, const CUtensorMap* tmdQ,
                                            const float* __restrict__ LSE, const float* __restrict__ Delta,
-                                           float* __restrict__ Delta_out, float scale, const Dq64Work& wk, int ow, int lane) {
+                                           float* __restrict__ Delta_out, float scale, const Dq64Work<kWindow>& wk, int ow,
+                                           int lane) {
     volatile int* abort_flag = &bars->abort_flag;
     const uint32_t lane_base = 32u * ow;
     const int r = lane_base + lane;
@@ -463,11 +487,11 @@ __device__ __forceinline__ void dq64_edges(uint8_t* smem, Dq64Bars* bars, uint32
     if (!kDelta && leader) bulk_wait_group<0>();  // dQ must be complete before the kernel ends
 }
 
-template <bool kCausal, bool kStrided, bool kDelta>
+template <bool kCausal, bool kStrided, bool kDelta, bool kWindow>
 __device__ __forceinline__ void dq64_body(const CUtensorMap* tmQ, const CUtensorMap* tmK, const CUtensorMap* tmV,
                                           const CUtensorMap* tmdO, const CUtensorMap* tmdQ, const float* __restrict__ LSE,
-                                          const float* __restrict__ Delta, float* __restrict__ Delta_out, const Dq64Work& wk,
-                                          float scale, int* __restrict__ dev_status) {
+                                          const float* __restrict__ Delta, float* __restrict__ Delta_out,
+                                          const Dq64Work<kWindow>& wk, float scale, int* __restrict__ dev_status) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     Dq64Bars* bars = reinterpret_cast<Dq64Bars*>(smem + kOffBar);
@@ -522,7 +546,7 @@ __device__ __forceinline__ void dq64_body(const CUtensorMap* tmQ, const CUtensor
     // kernel may take as long as it likes.
 
     if (warp == 0) {
-        if (lane == 0) dq64_producer<kStrided>(tmQ, tmK, tmV, tmdO, smem, bars, wk);
+        if (lane == 0) dq64_producer<kStrided, kWindow>(tmQ, tmK, tmV, tmdO, smem, bars, wk);
     } else if (warp == 1) {
         dq64_mma_sp<false, kDelta>(smem, bars, tmem_base, wk);
     } else if (warp == 2) {
@@ -530,9 +554,9 @@ __device__ __forceinline__ void dq64_body(const CUtensorMap* tmQ, const CUtensor
     } else if (warp == 3) {
         if constexpr (!kDelta) dq64_mma_dq(smem, bars, tmem_base, wk);
     } else if (warp >= 12) {
-        dq64_edges<kStrided, kDelta>(smem, bars, tmem_base, tmdQ, LSE, Delta, Delta_out, scale, wk, warp & 3, lane);
+        dq64_edges<kStrided, kDelta, kWindow>(smem, bars, tmem_base, tmdQ, LSE, Delta, Delta_out, scale, wk, warp & 3, lane);
     } else {
-        dq64_compute<kCausal, kDelta>(smem, bars, tmem_base, scale, wk, (warp - 4) >> 2, warp & 3, lane);
+        dq64_compute<kCausal, kDelta, kWindow>(smem, bars, tmem_base, scale, wk, (warp - 4) >> 2, warp & 3, lane);
     }
 
     tc_fence_before();
@@ -541,14 +565,14 @@ __device__ __forceinline__ void dq64_body(const CUtensorMap* tmQ, const CUtensor
     if (threadIdx.x == 0 && bars->abort_flag != 0) atomicExch(dev_status, kDevTimeout);
 }
 
-template <bool kCausal, bool kStrided>
+template <bool kCausal, bool kStrided, bool kWindow>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_dq64_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                  const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmdO,
                  const __grid_constant__ CUtensorMap tmdQ, const float* __restrict__ LSE, const float* __restrict__ Delta, int T,
-                 int BH, int H, uint32_t orders, int n_tiles, float scale, int* __restrict__ dev_status) {
+                 int BH, int H, uint32_t orders, int n_tiles, float scale, int* __restrict__ dev_status, const Window win) {
     dq64_body<kCausal, kStrided, false>(&tmQ, &tmK, &tmV, &tmdO, &tmdQ, LSE, Delta, nullptr,
-                                        Dq64Work{BH, n_tiles, T, H, orders, kCausal}, scale, dev_status);
+                                        Dq64Work<kWindow>{BH, n_tiles, T, H, orders, kCausal, win}, scale, dev_status);
 }
 
 template <bool kCausal>
@@ -558,7 +582,7 @@ attn_delta64_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_consta
                     const float* __restrict__ LSE, float* __restrict__ Delta, int T, int BH, int n_tiles, float scale,
                     int* __restrict__ dev_status) {
     dq64_body<kCausal, false, true>(&tmQ, &tmK, &tmV, &tmdO, nullptr, LSE, nullptr, Delta,
-                                    Dq64Work{BH, n_tiles, T, 1, 0u, kCausal}, scale, dev_status);
+                                    Dq64Work<false>{BH, n_tiles, T, 1, 0u, kCausal, Window{}}, scale, dev_status);
 }
 
 }  // namespace
@@ -567,26 +591,43 @@ cudaError_t configure_attn_dq64() {
     auto set = [](auto kernel) {
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
     };
-    cudaError_t e = set(attn_dq64_kernel<true, false>);
-    if (e == cudaSuccess) e = set(attn_dq64_kernel<true, true>);
-    if (e == cudaSuccess) e = set(attn_dq64_kernel<false, false>);
-    if (e == cudaSuccess) e = set(attn_dq64_kernel<false, true>);
+    cudaError_t e = set(attn_dq64_kernel<true, false, false>);
+    if (e == cudaSuccess) e = set(attn_dq64_kernel<true, true, false>);
+    if (e == cudaSuccess) e = set(attn_dq64_kernel<false, false, false>);
+    if (e == cudaSuccess) e = set(attn_dq64_kernel<false, true, false>);
+    if (e == cudaSuccess) e = set(attn_dq64_kernel<true, false, true>);
+    if (e == cudaSuccess) e = set(attn_dq64_kernel<true, true, true>);
     if (e == cudaSuccess) e = set(attn_delta64_kernel<true>);
     if (e == cudaSuccess) e = set(attn_delta64_kernel<false>);
     return e;
 }
 
-cudaError_t launch_attn_dq64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
-                             const CUtensorMap& tmdO, const CUtensorMap& tmdQ, bool strided, uint32_t orders,
-                             const float* LSE, const float* Delta, const AttnShape& s, int* dev_status, cudaStream_t stream) {
+namespace {
+cudaError_t launch_dq64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
+                        const CUtensorMap& tmdQ, bool strided, uint32_t orders, const float* LSE, const float* Delta,
+                        const AttnShape& s, const Window* win, int* dev_status, cudaStream_t stream) {
     const int n_tiles = (s.T + kBlockQ - 1) / kBlockQ, BH = s.B * s.H;
     const dim3 grid(static_cast<unsigned>(n_tiles) * BH);  // one CTA per item; those that do not start are taken over
     auto go = [&](auto kernel) {
         return launch_overlapped(kernel, grid, dim3(kThreads), kSmemBytes, stream, tmQ, tmK, tmV, tmdO, tmdQ, LSE, Delta, s.T, BH,
-                                 s.H, orders, n_tiles, s.scale, dev_status);
+                                 s.H, orders, n_tiles, s.scale, dev_status, win != nullptr ? *win : Window{});
     };
-    if (s.causal) return strided ? go(attn_dq64_kernel<true, true>) : go(attn_dq64_kernel<true, false>);
-    return strided ? go(attn_dq64_kernel<false, true>) : go(attn_dq64_kernel<false, false>);
+    if (win != nullptr) return strided ? go(attn_dq64_kernel<true, true, true>) : go(attn_dq64_kernel<true, false, true>);
+    if (s.causal) return strided ? go(attn_dq64_kernel<true, true, false>) : go(attn_dq64_kernel<true, false, false>);
+    return strided ? go(attn_dq64_kernel<false, true, false>) : go(attn_dq64_kernel<false, false, false>);
+}
+}  // namespace
+
+cudaError_t launch_attn_dq64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
+                             const CUtensorMap& tmdO, const CUtensorMap& tmdQ, bool strided, uint32_t orders,
+                             const float* LSE, const float* Delta, const AttnShape& s, int* dev_status, cudaStream_t stream) {
+    return launch_dq64(tmQ, tmK, tmV, tmdO, tmdQ, strided, orders, LSE, Delta, s, nullptr, dev_status, stream);
+}
+
+cudaError_t launch_window_dq64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
+                               const CUtensorMap& tmdQ, bool strided, uint32_t orders, const float* LSE, const float* Delta,
+                               const AttnShape& s, const Window& win, int* dev_status, cudaStream_t stream) {
+    return launch_dq64(tmQ, tmK, tmV, tmdO, tmdQ, strided, orders, LSE, Delta, s, &win, dev_status, stream);
 }
 
 cudaError_t launch_attn_delta64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,

@@ -15,10 +15,14 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <climits>
 #include <string>
 
 #include "../../include/nova_attn.h"
 #include "../../include/nova_lmhead.h"
+#include "../../include/nova_rope.h"
+#include "../../include/nova_window.h"
 
 namespace {
 
@@ -333,6 +337,200 @@ int lmhead_fwd(Args a) {  // X W targets logits lse loss workspace stream
         [&] { return nova_lmhead_fwd(xw[0], xw[1], targets, logits, stat[0], stat[1], m, n, k, ws.ptr, ws.bytes, st); });
 }
 
+// ---- nova_rope.py, nova_window.py.  Their calls run on the device of their tensors, which is one: the stream is that device's.
+struct OnDevice {
+    c10::DeviceIndex index;
+    c10::cuda::CUDAGuard guard;
+    explicit OnDevice(const at::Tensor& t) : index(t.device().index()), guard(index) {}
+    void same(const at::Tensor& t, const char* name) const {
+        if (t.device().index() != index)
+            raise(PyExc_ValueError, std::string(name) + " is on cuda:" + std::to_string(t.device().index()) + ", the first tensor on cuda:" +
+                                        std::to_string(index));
+    }
+    void* stream(PyObject* o) const {
+        if (o == Py_None) return c10::cuda::getCurrentCUDAStream(index).stream();
+        PyObject* d = PyObject_GetAttrString(o, "device_index");
+        if (!d) throw Failed{};
+        const long on = PyLong_AsLong(d);
+        Py_DECREF(d);
+        if (on == -1 && PyErr_Occurred()) throw Failed{};
+        if (on != index) raise(PyExc_ValueError, "the stream is of cuda:" + std::to_string(on) + ", the tensors are on cuda:" + std::to_string(index));
+        return ::stream(o);
+    }
+};
+
+int whole(PyObject* o, const char* name) {
+    PyObject* i = PyNumber_Index(o);
+    if (!i) throw Failed{};
+    int overflow = 0;
+    const long long v = PyLong_AsLongLongAndOverflow(i, &overflow);
+    Py_DECREF(i);
+    if (overflow != 0 || v > INT_MAX || v < INT_MIN) raise(PyExc_ValueError, std::string(name) + " is out of range");
+    return static_cast<int>(v);
+}
+
+const at::Tensor& cuda_bf16(PyObject* o, const char* name) {
+    const at::Tensor& t = tensor(o, name);
+    if (t.scalar_type() != at::kBFloat16 || !t.is_cuda() || t.dim() != 4 || (t.size(3) > 1 && t.stride(3) != 1))
+        raise(PyExc_TypeError,
+              std::string(name) + " must be a 4-D CUDA bf16 view [B,H,T,D] with a contiguous last dimension");
+    for (int i = 0; i < 4; ++i)
+        if (t.size(i) > INT_MAX) raise(PyExc_ValueError, std::string(name) + " has a dimension of 2^31 or more");
+    return t;
+}
+
+// Of what shape a view is, and its strides.  The stride of a dimension of size one is never used, and views have any number there:
+// one that the library takes stands in its place.
+struct View {
+    void* ptr;
+    nova_attn_strides st;
+    int n[4];
+    View(PyObject* o, const char* name) : View(cuda_bf16(o, name)) {}
+    explicit View(const at::Tensor& t) : ptr(data(t)), st{t.stride(0), t.stride(1), t.stride(2)} {
+        for (int i = 0; i < 4; ++i) n[i] = static_cast<int>(t.size(i));
+        const auto odd = [](long long s, long long least) { return s < least || (s & 7) != 0; };
+        if (n[2] == 1 && odd(st.token, n[3])) st.token = (n[3] + 7) / 8 * 8;
+        if (n[1] == 1 && odd(st.head, 8)) st.head = st.token * n[2];
+        if (n[0] == 1 && odd(st.batch, 8)) st.batch = std::max(st.head * n[1], st.token * n[2]);
+    }
+    // the shape [B,H,T,D]; a head count of -1 is any
+    View(PyObject* o, const char* name, const OnDevice& dev, int B, int H, int T, int D) : View(o, name) {
+        dev.same(THPVariable_Unpack(o), name);
+        if (n[0] != B || (H >= 0 && n[1] != H) || n[2] != T || n[3] != D)
+            raise(PyExc_ValueError, std::string(name) + " has shape " + shape_text(THPVariable_Unpack(o).sizes()) + ", expected " +
+                                        (H >= 0 ? shape_text({B, H, T, D})
+                                                : "(" + std::to_string(B) + ", any, " + std::to_string(T) + ", " + std::to_string(D) + ")"));
+    }
+};
+
+float* f32_on(PyObject* o, const char* name, const OnDevice& dev, at::IntArrayRef want) {
+    float* p = f32(o, name, want);
+    dev.same(THPVariable_Unpack(o), name);
+    return p;
+}
+
+int rope(Args a) {  // Q K Q_out K_out inv_freq positions interleaved amplitude backward stream
+    const View q(a[0], "Q");
+    const OnDevice dev(THPVariable_Unpack(a[0]));
+    const int B = q.n[0], H = q.n[1], T = q.n[2], D = q.n[3];
+    const View qo(a[2], "Q_out", dev, B, H, T, D);
+    const bool with_k = a[1] != Py_None;
+    if (with_k != (a[3] != Py_None)) raise(PyExc_TypeError, "K and K_out must both be given, or both be None");
+    const View k = with_k ? View(a[1], "K", dev, B, -1, T, D) : q;
+    const View ko = with_k ? View(a[3], "K_out", dev, B, k.n[1], T, D) : q;
+    const at::Tensor& f = tensor(a[4], "inv_freq");
+    if (f.scalar_type() != at::kFloat || !f.is_cuda() || !f.is_contiguous() || f.dim() != 1)
+        raise(PyExc_TypeError, "inv_freq must be a contiguous 1-D CUDA fp32 tensor [rotary / 2]");
+    dev.same(f, "inv_freq");
+    if (2 * f.size(0) > D) raise(PyExc_ValueError, "inv_freq has more than D / 2 numbers");
+    const int rotary = static_cast<int>(2 * f.size(0));
+    const int* pos = nullptr;
+    long long pos_stride = 0;
+    if (a[5] != Py_None) {
+        const at::Tensor& p = tensor(a[5], "positions");
+        const bool shared = p.dim() == 1;
+        if (p.scalar_type() != at::kInt || !p.is_cuda() || (p.dim() != 1 && p.dim() != 2) || (T > 1 && p.stride(-1) != 1))
+            raise(PyExc_TypeError, "positions must be a CUDA int32 tensor [T] or [B,T] with a contiguous last dimension, or None");
+        dev.same(p, "positions");
+        if (p.size(-1) != T || (!shared && p.size(0) != B))
+            raise(PyExc_ValueError, "positions has shape " + shape_text(p.sizes()) + ", expected " + shape_text({B, T}) + " or " + shape_text({T}));
+        pos = static_cast<const int*>(data(p));
+        pos_stride = shared || B == 1 ? 0 : p.stride(0);
+    }
+    const int interleaved = truth(a[6]);
+    const float amplitude = real(a[7]);
+    const int backward = truth(a[8]);
+    void* st = dev.stream(a[9]);
+    return without_gil([&] {
+        return (backward ? nova_rope_bwd : nova_rope_fwd)(q.ptr, with_k ? k.ptr : nullptr, qo.ptr, with_k ? ko.ptr : nullptr,
+                                                          static_cast<const float*>(data(f)), pos, B, H, k.n[1], T, D, rotary,
+                                                          interleaved, amplitude, pos_stride, &q.st, &k.st, &qo.st, &ko.st, st);
+    });
+}
+
+int window_fwd(Args a) {  // Q K V O O_rest LSE scale window sinks stream
+    const View q(a[0], "Q");
+    const OnDevice dev(THPVariable_Unpack(a[0]));
+    const int B = q.n[0], H = q.n[1], T = q.n[2], D = q.n[3];
+    const View k(a[1], "K", dev, B, -1, T, D), v(a[2], "V", dev, B, k.n[1], T, D), o(a[3], "O", dev, B, H, T, D);
+    void* rest = nullptr;
+    if (a[4] != Py_None) {
+        const View r(a[4], "O_rest", dev, B, H, T, D);
+        if (r.st.batch != o.st.batch || r.st.head != o.st.head || r.st.token != o.st.token)
+            raise(PyExc_ValueError, "O_rest must have the strides of O");
+        rest = r.ptr;
+    }
+    float* lse = f32_on(a[5], "LSE", dev, {B, H, T});
+    const float scale = real(a[6]);
+    const int window = whole(a[7], "window"), sinks = whole(a[8], "sinks");
+    void* st = dev.stream(a[9]);
+    return without_gil([&] {
+        return nova_window_fwd(q.ptr, k.ptr, v.ptr, o.ptr, rest, lse, B, H, k.n[1], T, D, window, sinks, &q.st, &k.st, &v.st, &o.st,
+                               scale, st);
+    });
+}
+
+int window_preprocess(Args a) {  // O O_rest dO Delta stream
+    const View o(a[0], "O");
+    const OnDevice dev(THPVariable_Unpack(a[0]));
+    const int B = o.n[0], H = o.n[1], T = o.n[2], D = o.n[3];
+    void* rest = nullptr;
+    if (a[1] != Py_None) {
+        const View r(a[1], "O_rest", dev, B, H, T, D);
+        if (r.st.batch != o.st.batch || r.st.head != o.st.head || r.st.token != o.st.token)
+            raise(PyExc_ValueError, "O_rest must have the strides of O");
+        rest = r.ptr;
+    }
+    const View g(a[2], "dO", dev, B, H, T, D);
+    float* delta = f32_on(a[3], "Delta", dev, {B, H, T});
+    void* st = dev.stream(a[4]);
+    return without_gil([&] { return nova_window_bwd_preprocess(o.ptr, rest, g.ptr, delta, B, H, T, D, &o.st, &g.st, st); });
+}
+
+int window_bwd(Args a) {  // Q K V dO LSE Delta dQ dK dV scale window sinks workspace stream
+    const View q(a[0], "Q");
+    const OnDevice dev(THPVariable_Unpack(a[0]));
+    const int B = q.n[0], H = q.n[1], T = q.n[2], D = q.n[3];
+    const View k(a[1], "K", dev, B, -1, T, D), v(a[2], "V", dev, B, k.n[1], T, D), g(a[3], "dO", dev, B, H, T, D);
+    const int KV = k.n[1];
+    const View dq(a[6], "dQ", dev, B, H, T, D), dk(a[7], "dK", dev, B, KV, T, D), dv(a[8], "dV", dev, B, KV, T, D);
+    float *lse = f32_on(a[4], "LSE", dev, {B, H, T}), *delta = f32_on(a[5], "Delta", dev, {B, H, T});
+    const float scale = real(a[9]);
+    const int window = whole(a[10], "window"), sinks = whole(a[11], "sinks");
+    void* st = dev.stream(a[13]);
+    if (a[12] != Py_None) dev.same(tensor(a[12], "workspace"), "workspace");
+    const Workspace ws(a[12], nova_window_bwd_workspace_bytes(B, H, KV, T, D, window, sinks), a[0], st);
+    return without_gil([&] {
+        return nova_window_bwd(q.ptr, k.ptr, v.ptr, g.ptr, lse, delta, dq.ptr, dk.ptr, dv.ptr, B, H, KV, T, D, window, sinks, &q.st,
+                               &k.st, &v.st, &g.st, &dq.st, &dk.st, &dv.st, scale, ws.ptr, ws.bytes, st);
+    });
+}
+
+int window_decode(Args a) {  // Q K V lengths O LSE scale window sinks workspace stream
+    const View q(a[0], "Q");
+    const OnDevice dev(THPVariable_Unpack(a[0]));
+    const int B = q.n[0], H = q.n[1], D = q.n[3];
+    if (q.n[2] != 1) raise(PyExc_ValueError, "Q must hold one token per sequence, [B,H,1,D]");
+    const View k(a[1], "K");
+    const int KV = k.n[1], T = k.n[2];
+    const View k2(a[1], "K", dev, B, KV, T, D), v(a[2], "V", dev, B, KV, T, D), o(a[4], "O", dev, B, H, 1, D);
+    const at::Tensor& l = tensor(a[3], "lengths");
+    if (l.scalar_type() != at::kInt || !l.is_cuda() || !l.is_contiguous() || l.sizes() != at::IntArrayRef({B}))
+        raise(PyExc_TypeError, "lengths must be a contiguous CUDA int32 tensor [B]");
+    dev.same(l, "lengths");
+    float* lse = f32_on(a[5], "LSE", dev, {B, H, 1});
+    const float scale = real(a[6]);
+    const int window = whole(a[7], "window"), sinks = whole(a[8], "sinks");
+    void* st = dev.stream(a[10]);
+    if (a[9] != Py_None) dev.same(tensor(a[9], "workspace"), "workspace");
+    const Workspace ws(a[9], nova_window_decode_workspace_bytes(B, H, KV, T, D, window, sinks), a[0], st);
+    const int* lengths = static_cast<const int*>(data(l));
+    return without_gil([&] {
+        return nova_window_decode(q.ptr, k2.ptr, v.ptr, lengths, o.ptr, lse, B, H, KV, T, D, window, sinks, &q.st, &k2.st, &v.st,
+                                  &o.st, scale, ws.ptr, ws.bytes, st);
+    });
+}
+
 template <int (*F)(Args), int kCount>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != kCount) {
@@ -361,6 +559,11 @@ PyMethodDef methods[] = {
     NOVA_ENTRY("bwd_deterministic", bwd_deterministic, 12),
     NOVA_ENTRY("bwd_strided", bwd_strided, 13),
     NOVA_ENTRY("lmhead_fwd", lmhead_fwd, 8),
+    NOVA_ENTRY("rope", rope, 10),
+    NOVA_ENTRY("window_fwd", window_fwd, 10),
+    NOVA_ENTRY("window_preprocess", window_preprocess, 5),
+    NOVA_ENTRY("window_bwd", window_bwd, 14),
+    NOVA_ENTRY("window_decode", window_decode, 11),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

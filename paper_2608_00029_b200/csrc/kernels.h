@@ -25,6 +25,52 @@ struct TensorStrides {
     long long b, h, t;
 };
 
+// The window of nova_window.h: query i keeps key j if j <= i and (i - j < window or j < sinks).  Both at most T; `group` query heads
+// share a key/value head.  The attention kernels have builds of their own for it (kWindow).
+struct Window {
+    int window, sinks, group;
+};
+
+// The key tiles of `unit` keys that the queries q0 .. q0 + rows - 1 of T keep anything of, numbered: those of the sinks that lie
+// before the window, then the window's.
+struct KeySpan {
+    int sinks, skip, n;
+    __host__ __device__ __forceinline__ int at(int j) const { return j < sinks ? j : j + skip; }
+};
+__host__ __device__ __forceinline__ KeySpan key_span(const Window& w, int q0, int rows, int T, int unit) {
+    const int last = (q0 + rows < T ? q0 + rows : T) - 1, first = q0 - w.window + 1;
+    const int lo = first > 0 ? first / unit : 0, hi = last / unit + 1;
+    const int all = (w.sinks + unit - 1) / unit, sinks = all < lo ? all : lo;
+    return KeySpan{sinks, lo - sinks, sinks + hi - lo};
+}
+// The query steps of `unit` rows of which anything keeps a key of the tile k0 .. k0 + keys - 1: the first, and how many.
+__host__ __device__ __forceinline__ int query_steps(const Window& w, int k0, int keys, int T, int unit) {
+    const int reach = (k0 + keys < T ? k0 + keys : T) - 1 + w.window;  // past the last query that a key outside the sinks has
+    const int end = k0 < w.sinks || reach > T ? T : reach;
+    return (end - 1) / unit + 1 - k0 / unit;
+}
+
+#ifdef __CUDACC__
+// Bits 0 .. n - 1 of 64.
+__device__ __forceinline__ uint64_t bits_below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }
+// Which of the 64 keys from k0 on query `row` keeps (bit i: key k0 + i).
+__device__ __forceinline__ uint64_t kept_keys(const Window& w, int row, int k0) {
+    return bits_below(row + 1 - k0) & (~bits_below(row + 1 - w.window - k0) | bits_below(w.sinks - k0));
+}
+// Is there anything among the 64 keys from k0 on that one of the queries q0 .. q1 does not keep?
+__device__ __forceinline__ bool any_dropped(const Window& w, int q0, int q1, int k0) {
+    return k0 + 63 > q0 || (q1 - k0 >= w.window && k0 + 64 > w.sinks);
+}
+// Is there anything among the 64 queries from q0 on that does not keep one of the keys k0 .. k0 + 127?
+__device__ __forceinline__ bool any_dropping(const Window& w, int k0, int q0) {
+    return q0 < k0 + kBlockK - 1 || (q0 + 63 - k0 >= w.window && k0 + kBlockK > w.sinks);
+}
+// Which of the 64 queries from q0 on keep `key`.
+__device__ __forceinline__ uint64_t keeping_queries(const Window& w, int key, int q0) {
+    return ~bits_below(key - q0) & (key < w.sinks ? ~0ull : bits_below(key + w.window - q0));
+}
+#endif
+
 // Records a CUDA error code for nova_attn_last_cuda_error() of the calling thread and returns
 // NOVA_ATTN_ERR_CUDA; for the entry points that live outside api.cu.
 int record_cuda_error(int code);
@@ -63,9 +109,14 @@ inline cudaError_t launch_overlapped(void (*kernel)(KArgs...), dim3 grid, dim3 b
 cudaError_t launch_attn_fwd(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
                             const CUtensorMap& tmO, bool strided, uint32_t orders, float* LSE, const AttnShape& s,
                             int num_sms, long long wait_limit, int inject, int* dev_status, cudaStream_t stream);
+// With the window: K and V maps have B * H / win.group heads; `rest` null or a tensor with O's strides `so`.
+cudaError_t launch_window_fwd(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmO,
+                              bool strided, uint32_t orders, float* LSE, __nv_bfloat16* rest, const TensorStrides& so,
+                              const AttnShape& s, const Window& win, int num_sms, int* dev_status, cudaStream_t stream);
 cudaError_t configure_attn_fwd();
 
-cudaError_t launch_attn_bwd_preprocess(const __nv_bfloat16* O, const __nv_bfloat16* dO, float* Delta,
+// `rest`: what rounding took from O, with its strides, or null.
+cudaError_t launch_attn_bwd_preprocess(const __nv_bfloat16* O, const __nv_bfloat16* rest, const __nv_bfloat16* dO, float* Delta,
                                        const AttnShape& s, const TensorStrides& so, const TensorStrides& sdo,
                                        int num_sms, cudaStream_t stream);
 
@@ -82,6 +133,10 @@ cudaError_t launch_attn_dq(const CUtensorMap& tmQ, const CUtensorMap& tmK, const
                            const CUtensorMap& tmdO, const CUtensorMap& tmdQ, bool strided, uint32_t orders,
                            const float* LSE, const float* Delta, const AttnShape& s, int num_sms, int* dev_status,
                            cudaStream_t stream);
+// With the window (D = 128), as in the forward.
+cudaError_t launch_window_dq(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
+                             const CUtensorMap& tmdQ, bool strided, uint32_t orders, const float* LSE, const float* Delta,
+                             const AttnShape& s, const Window& win, int num_sms, int* dev_status, cudaStream_t stream);
 cudaError_t configure_attn_dq();
 // The same two at D = 64, with their operands in tensor memory (attn_dq64.cu).  The same bits of Delta.
 cudaError_t launch_attn_delta64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
@@ -90,6 +145,9 @@ cudaError_t launch_attn_delta64(const CUtensorMap& tmQ, const CUtensorMap& tmK, 
 cudaError_t launch_attn_dq64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
                              const CUtensorMap& tmdO, const CUtensorMap& tmdQ, bool strided, uint32_t orders,
                              const float* LSE, const float* Delta, const AttnShape& s, int* dev_status, cudaStream_t stream);
+cudaError_t launch_window_dq64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
+                               const CUtensorMap& tmdQ, bool strided, uint32_t orders, const float* LSE, const float* Delta,
+                               const AttnShape& s, const Window& win, int* dev_status, cudaStream_t stream);
 cudaError_t configure_attn_dq64();
 
 // The dK/dV half of the two-kernel backward at D = 128 (attn_dkdv.cu): Q and dO maps with boxes of kKeyStep rows, the
@@ -98,6 +156,11 @@ cudaError_t launch_attn_dkdv(const CUtensorMap& tmQ, const CUtensorMap& tmK, con
                              const CUtensorMap& tmdO, const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided,
                              uint32_t orders, const float* LSE, const float* Delta, const AttnShape& s, int num_sms,
                              int* dev_status, cudaStream_t stream);
+// With the window: dK and dV have the heads of K and V, an item all query heads that share its key/value head.
+cudaError_t launch_window_dkdv(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
+                               const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided, uint32_t orders, const float* LSE,
+                               const float* Delta, const AttnShape& s, const Window& win, int num_sms, int* dev_status,
+                               cudaStream_t stream);
 cudaError_t configure_attn_dkdv();
 // The same at D = 64 (attn_dkdv64.cu).  `terms`: the row terms of every query as launch_row_terms64 leaves them (32 bytes for
 // each of B * H * ceil(T / 64) * 64 rows, 16-byte aligned), or null: the kernel makes them itself (plain layout only).  Goes out
@@ -107,6 +170,10 @@ cudaError_t launch_attn_dkdv64(const CUtensorMap& tmQ, const CUtensorMap& tmK, c
                                const CUtensorMap& tmdO, const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided,
                                uint32_t orders, const float* LSE, const float* Delta, const void* terms, const AttnShape& s,
                                int* dev_status, cudaStream_t stream);
+cudaError_t launch_window_dkdv64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
+                                 const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided, uint32_t orders, const float* LSE,
+                                 const float* Delta, const void* terms, const AttnShape& s, const Window& win, int* dev_status,
+                                 cudaStream_t stream);
 cudaError_t configure_attn_dkdv64();
 
 // Heads that the items of the kernels at D=128 are taken in together: enough items for two rounds of the SMs, and no more
