@@ -1,8 +1,10 @@
 // Rotary positions of queries and keys (include/nova_rope.h).
 //
-// Memory bound: 4 bytes an element, and a sine and a cosine per token and pair, which all heads of the token share.  So a thread
-// keeps one place in the head (8 dimensions, and in the half layout the 8 that they are paired with) of one token and walks
-// over heads: it makes its angles once and then only streams, the 16-byte loads of four heads in flight.
+// Memory bound: 4 bytes an element, and a sine and a cosine per token and pair, which all heads of the token share.  A block has
+// a few tokens and all their heads: it makes the tokens' angles once, one or two a thread, into shared memory, while the
+// first elements are on their way.  A thread keeps one place in the head (8 dimensions, and in the half layout the 8 that they
+// are paired with) of one token and walks over heads with 16-byte accesses, four heads in flight.
+#include <algorithm>
 #include <cmath>
 
 #include "../../../include/nova_rope.h"
@@ -13,7 +15,9 @@ namespace nova {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kHeadsInFlight = 4;
+constexpr int kMaxAngles = 2048;  // of a block
+// Heads of which a thread has the loads out together: 128 bytes of them in both layouts.
+__host__ __device__ constexpr int heads_in_flight(bool interleaved) { return interleaved ? 8 : 4; }
 
 struct RopeArgs {
     const uint16_t* in[2];  // Q, K
@@ -21,11 +25,11 @@ struct RopeArgs {
     TensorStrides sin[2], sout[2];
     const float* inv_freq;
     const int* positions;
-    long long position_stride, units;
-    int heads[2], T, rotary, rot_chunks, chunks, groups;
-    float amplitude;  // its sign is that of the forward
-    float sign;       // -1: backward
-    bool heads_inside, wide;
+    long long position_stride;
+    int heads[2], T, rows, rotary, rot_chunks, chunks, groups, tokens;  // rows: B * T; tokens: of a block
+    float amplitude;
+    float sign;  // -1: backward
+    bool heads_inside;
 };
 
 template <int V>
@@ -59,81 +63,87 @@ __device__ __forceinline__ typename Vec<V>::type narrow(const float (&f)[V]) {
 }
 
 // V elements to an access.  Half layout: places d and d + rotary/2 of a pair are V neighbours each; interleaved: V neighbours
-// are V/2 pairs.  A unit is a chunk of V places (the last ones are copied), a token and a group of heads; where the
-// heads of a token lie inside it, units next to each other take its heads in turn.
+// are V/2 pairs.  A unit is a chunk of V places (the last ones are copied), a token and a group of heads; units next to each
+// other have the chunks of one head and then, whichever lies closer, the token's other heads or the head's other tokens.
 template <int V, bool kInterleaved>
 __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeArgs a) {
     using T4 = typename Vec<V>::type;
     constexpr int kAngles = kInterleaved ? V / 2 : V;
+    constexpr int kHeadsInFlight = heads_in_flight(kInterleaved);
+    __shared__ float2 angles[kMaxAngles];  // [token of the block][pair] cosine, sine
     griddep_launch_dependents();
-    const long long u = static_cast<long long>(blockIdx.x) * kThreads + threadIdx.x;
-    const bool any = u < a.units;
-    int c = 0, t = 0, g = 0, b = 0;
-    if (a.wide) {
-        long long r = u / a.chunks;
-        c = static_cast<int>(u - r * a.chunks);
-        const int inner = a.heads_inside ? a.groups : a.T, outer = a.heads_inside ? a.T : a.groups;
-        long long r2 = r / inner;
-        const int x = static_cast<int>(r - r2 * inner);
-        b = static_cast<int>(r2 / outer);
-        const int y = static_cast<int>(r2 - static_cast<long long>(b) * outer);
-        t = a.heads_inside ? y : x;
-        g = a.heads_inside ? x : y;
-    } else {
-        const uint32_t u32 = static_cast<uint32_t>(u), r = u32 / a.chunks;
-        c = static_cast<int>(u32 - r * a.chunks);
-        const uint32_t inner = a.heads_inside ? a.groups : a.T, outer = a.heads_inside ? a.T : a.groups;
-        const uint32_t r2 = r / inner, x = r - r2 * inner;
-        b = static_cast<int>(r2 / outer);
-        const uint32_t y = r2 - b * outer;
-        t = a.heads_inside ? y : x;
-        g = a.heads_inside ? x : y;
-    }
-    griddep_wait();
-    if (!any) return;
+    const int row0 = blockIdx.x * a.tokens, n_tokens = min(a.tokens, a.rows - row0), pairs = a.rotary / 2;
+    const int units = n_tokens * a.chunks * a.groups, heads = a.heads[0] + a.heads[1];
 
-    const bool turns = c < a.rot_chunks;
-    float co[kAngles], si[kAngles];
-    int d = c * V, d2 = d;  // first place, and in the half layout that of the other ends of the pairs
-    if (turns) {
-        const double pos = a.positions != nullptr ? __ldg(a.positions + b * a.position_stride + t) : t;
-        const int pair = kInterleaved ? d / 2 : d;
+    int tok, g, d, d2;  // token of the block, group, first place, and in the half layout that of the other ends of the pairs
+    bool turns;
+    const uint16_t* in[2];
+    uint16_t* out[2];
+    T4 x4[kHeadsInFlight], y4[kHeadsInFlight];
+    auto locate = [&](int u) {
+        const int r = u / a.chunks, c = u - r * a.chunks;
+        const int inner = a.heads_inside ? a.groups : n_tokens, y = r / inner, x = r - y * inner;
+        tok = a.heads_inside ? y : x, g = a.heads_inside ? x : y;
+        const int b = (row0 + tok) / a.T, t = row0 + tok - b * a.T;
+        turns = c < a.rot_chunks;
+        d = kInterleaved || turns ? c * V : a.rotary + (c - a.rot_chunks) * V;
+        d2 = d + pairs;
 #pragma unroll
-        for (int i = 0; i < kAngles; ++i) {
-            const double turn = pos * static_cast<double>(__ldg(a.inv_freq + pair + i)) * 0.15915494309189535;  // 1 / 2 pi
-            sincospif(2.0f * static_cast<float>(turn - rint(turn)), &si[i], &co[i]);
-            si[i] *= a.amplitude * a.sign;
-            co[i] *= a.amplitude;
+        for (int w = 0; w < 2; ++w) {
+            in[w] = a.in[w] + b * a.sin[w].b + t * a.sin[w].t - w * a.heads[0] * a.sin[w].h;
+            out[w] = a.out[w] + b * a.sout[w].b + t * a.sout[w].t - w * a.heads[0] * a.sout[w].h;
         }
-        if (!kInterleaved) d2 = d + a.rotary / 2;
-    } else if (!kInterleaved) {
-        d = d2 = a.rotary + (c - a.rot_chunks) * V;
-    }
+    };
+    // heads h0, h0 + groups, ... of both tensors, those of Q first (the pointers of K are those of its head -H)
+    auto load = [&](int h0) {
+#pragma unroll
+        for (int k = 0; k < kHeadsInFlight; ++k) {
+            const int h = h0 + k * a.groups;
+            if (h >= heads) break;
+            const uint16_t* const p = h < a.heads[0] ? in[0] + h * a.sin[0].h : in[1] + h * a.sin[1].h;
+            x4[k] = *reinterpret_cast<const T4*>(p + d);
+            if (!kInterleaved && turns) y4[k] = *reinterpret_cast<const T4*>(p + d2);
+        }
+    };
 
+    griddep_wait();
+    const bool any = threadIdx.x < units;
+    if (any) {
+        locate(threadIdx.x);
+        load(g);
+    }
+    for (int x = threadIdx.x; x < n_tokens * pairs; x += kThreads) {
+        const int k = x / pairs, i = x - k * pairs;
+        const int b = (row0 + k) / a.T, t = row0 + k - b * a.T;
+        const double pos = a.positions != nullptr ? __ldg(a.positions + b * a.position_stride + t) : t;
+        const double turn = pos * static_cast<double>(__ldg(a.inv_freq + i)) * 0.15915494309189535;  // 1 / 2 pi
+        float s, c;
+        sincospif(2.0f * static_cast<float>(turn - rint(turn)), &s, &c);
+        angles[x] = make_float2(c * a.amplitude, s * a.amplitude * a.sign);
+    }
+    __syncthreads();
+
+    for (int u = threadIdx.x; u < units; u += kThreads) {
+        if (u >= kThreads) {
+            locate(u);
+            load(g);
+        }
+        float co[kAngles], si[kAngles];
+        if (turns) {
+            const float2* const p = angles + tok * pairs + (kInterleaved ? d / 2 : d);
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        const TensorStrides si_ = a.sin[which], so_ = a.sout[which];
-        const uint16_t* const in = a.in[which] + b * si_.b + t * si_.t;
-        uint16_t* const out = a.out[which] + b * so_.b + t * so_.t;
-        // heads are dealt out over the groups through both tensors
-        const int first = which == 0 ? g : (g - a.heads[0] % a.groups + a.groups) % a.groups;
-        for (int h0 = first; h0 < a.heads[which]; h0 += kHeadsInFlight * a.groups) {
-            T4 x[kHeadsInFlight], y[kHeadsInFlight];
+            for (int i = 0; i < kAngles; ++i) co[i] = p[i].x, si[i] = p[i].y;
+        }
+        for (int h0 = g; h0 < heads; h0 += kHeadsInFlight * a.groups) {
+            if (h0 != g) load(h0);
 #pragma unroll
             for (int k = 0; k < kHeadsInFlight; ++k) {
                 const int h = h0 + k * a.groups;
-                if (h < a.heads[which]) {
-                    x[k] = *reinterpret_cast<const T4*>(in + h * si_.h + d);
-                    if (!kInterleaved && turns) y[k] = *reinterpret_cast<const T4*>(in + h * si_.h + d2);
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < kHeadsInFlight; ++k) {
-                const int h = h0 + k * a.groups;
-                if (h >= a.heads[which]) break;
+                if (h >= heads) break;
+                uint16_t* const to = h < a.heads[0] ? out[0] + h * a.sout[0].h : out[1] + h * a.sout[1].h;
                 if (turns) {
                     float p[V];
-                    widen<V>(x[k], p);
+                    widen<V>(x4[k], p);
                     if constexpr (kInterleaved) {
 #pragma unroll
                         for (int i = 0; i < V; i += 2) {
@@ -143,18 +153,18 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
                         }
                     } else {
                         float q[V];
-                        widen<V>(y[k], q);
+                        widen<V>(y4[k], q);
 #pragma unroll
                         for (int i = 0; i < V; ++i) {
                             const float p0 = p[i];
                             p[i] = p0 * co[i] - q[i] * si[i];
                             q[i] = q[i] * co[i] + p0 * si[i];
                         }
-                        *reinterpret_cast<T4*>(out + h * so_.h + d2) = narrow<V>(q);
+                        *reinterpret_cast<T4*>(to + d2) = narrow<V>(q);
                     }
-                    x[k] = narrow<V>(p);
+                    x4[k] = narrow<V>(p);
                 }
-                *reinterpret_cast<T4*>(out + h * so_.h + d) = x[k];
+                *reinterpret_cast<T4*>(to + d) = x4[k];
             }
         }
     }
@@ -203,17 +213,20 @@ int rope(const void* Q, const void* K, void* Qo, void* Ko, const float* inv_freq
     const bool in_place = Q == Qo && (!K || K == Ko);
     a.chunks = a.rot_chunks + (in_place ? 0 : (D - rotary) / v);
     a.heads_inside = a.sin[0].h < a.sin[0].t;
-    // Groups of heads: threads for two rounds of the chip, if there are heads enough.
+    // Heads in flight to a thread, if that leaves 512 threads for every SM (24 heads, R=64, half layout, B=8, T=1024: 9.7 us with
+    // four, 11.2 with all of them to a thread); tokens for whole blocks, if that leaves a block for every SM.
     const int heads = H + H_kv;
-    const long long places = static_cast<long long>(B) * T * a.chunks, wanted = 2048ll * 2 * st->num_sms;
-    long long groups = (wanted + places - 1) / places;
-    a.groups = static_cast<int>(groups < heads ? groups : heads);
-    a.units = places * a.groups;
-    a.wide = a.units >= (1ll << 31);
-    const long long blocks = (a.units + kThreads - 1) / kThreads;
-    if (blocks > 0x7fffffffll) return NOVA_ATTN_ERR_SHAPE;
+    a.rows = B * T;
+    const long long places = static_cast<long long>(a.rows) * a.chunks;
+    const int flight = heads_in_flight(interleaved != 0);
+    const int per_thread = places * heads >= 512ll * flight * st->num_sms ? flight : 1;
+    a.groups = std::max(1, std::min(kThreads / a.chunks, (heads + per_thread - 1) / per_thread));
+    int tokens = std::max(1, kThreads / (a.chunks * a.groups));
+    tokens = std::min(tokens, std::max(1, kMaxAngles / (rotary / 2)));
+    a.tokens = std::max(1, std::min(tokens, (a.rows + st->num_sms - 1) / st->num_sms));
+    const int blocks = (a.rows + a.tokens - 1) / a.tokens;
     auto go = [&](auto kernel) {
-        return launch_overlapped(kernel, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, static_cast<cudaStream_t>(stream), a);
+        return launch_overlapped(kernel, dim3(blocks), dim3(kThreads), 0, static_cast<cudaStream_t>(stream), a);
     };
     cudaError_t e;
     if (interleaved)
