@@ -77,6 +77,7 @@ int device_state(DeviceState** out) {
         if (e == cudaSuccess) e = configure_attn_dkdv64();
         if (e == cudaSuccess) e = configure_lmhead();
         if (e == cudaSuccess) e = configure_lmhead_rows();
+        if (e == cudaSuccess) e = configure_window_fwd();
         if (e == cudaSuccess) e = cudaGetSymbolAddress(reinterpret_cast<void**>(&st.dev_status), g_dev_status);
         if (e != cudaSuccess) { st.status = fail_cuda(e); return st.status; }
     }

@@ -81,22 +81,15 @@ constexpr int kWorkConsumers = 1 + 8;  // UMMA issuer warp + 8 softmax warps
 // one block to the next (184 -> 171 us at B=16, H=32, T=1024, 150 -> 139 us at B=2, H=16, T=4096; D=64, with half the
 // bytes per head, gained nothing).  kSingle: 128-row blocks, tile A alone.
 // kOwn: O leaves through buffers of its own (D=128, pairs of tiles, more items than SMs).
-// kWindow: only single tiles; two stages of Q at D=128 as well, in the place of tile B's buffer, because items are short.
-template <int D, bool kSingle, bool kOwn, bool kWindow>
+template <int D, bool kSingle, bool kOwn>
 struct FwdWork {
     static constexpr bool kOwnStage = kOwn;
-    static constexpr int kQStages = kWindow ? 2 : FwdCfg<D>::kQStages;
-    static constexpr int kQStride = (kWindow && D == 128 ? 1 : 2) * FwdCfg<D>::kTileBytes;  // from stage to stage
-    // kSingle: the groups' sums, in the Q buffer of a tile B
-    static constexpr int kOffSums = kWindow && D == 128 ? FwdCfg<D>::kOffO : FwdCfg<D>::kOffQ + FwdCfg<D>::kTileBytes;
     static constexpr bool kChunks = (D == 128) && !kSingle;
     static constexpr int kRows = kSingle ? kBlockQ : kBlockRows;
     static constexpr int kTiles = kRows / kBlockQ;
     int n_items, BH, n_blocks, n_kv_all, T, H, chunk;
     uint32_t orders;  // coordinate orders of the Q, K, V, O tensor maps, four bits each
     bool causal;
-    Window win;
-    __device__ __forceinline__ KeySpan span(int blk) const { return key_span(win, blk * kBlockQ, kBlockQ, T, kBlockK); }
     // Item `idx`: block index, head, and the number of key tiles each query tile visits
     // (0 if the tile lies entirely past the end of the sequence).
     __device__ __forceinline__ void get(int idx, int* blk, int* bh, int* n_a, int* n_b) const {
@@ -115,11 +108,6 @@ struct FwdWork {
             *blk = n_blocks - 1 - idx / BH;
             *bh = idx % BH;
         }
-        if constexpr (kWindow) {
-            *n_a = span(*blk).n;
-            *n_b = 0;
-            return;
-        }
         const int qt_a = kTiles * (*blk), qt_b = qt_a + 1;
         // causal clamp of the key loop: tile qt visits key tiles 0..qt
         *n_a = causal ? min(qt_a + 1, n_kv_all) : n_kv_all;
@@ -127,7 +115,7 @@ struct FwdWork {
     }
 };
 
-template <int D, bool kStrided, bool kWindow, typename Work>
+template <int D, bool kStrided, typename Work>
 __device__ __forceinline__ void fwd_producer(const CUtensorMap* tmQ, const CUtensorMap* tmK,
                                              const CUtensorMap* tmV, uint8_t* smem, FwdBars* bars,
                                              const Work& wk, long long limit, int inject) {
@@ -145,11 +133,8 @@ __device__ __forceinline__ void fwd_producer(const CUtensorMap* tmQ, const CUten
         int blk, bh, n_a, n_b;
         wk.get(item, &blk, &bh, &n_a, &n_b);
         const int head = kStrided ? bh % wk.H : 0, batch = kStrided ? bh / wk.H : 0;
-        // with the window: the key/value head that the query head shares, and the tiles in its reach
-        const int kv_head = kWindow ? head / wk.win.group : head, kv_bh = kWindow ? bh / wk.win.group : bh;
-        const KeySpan span = kWindow ? wk.span(blk) : KeySpan{0, 0, 0};
-        const int qs = w % Work::kQStages;
-        const uint32_t qph = (w / Work::kQStages) & 1;
+        const int qs = w % Cfg::kQStages;
+        const uint32_t qph = (w / Cfg::kQStages) & 1;
         ok = mbar_wait(&bars->q_empty[qs], qph ^ 1, abort_flag, limit);
         if (!ok) break;
         mbar_expect_tx(&bars->q_full[qs], Work::kTiles * Cfg::kTileBytes);  // rows past T arrive as zeros
@@ -158,13 +143,12 @@ __device__ __forceinline__ void fwd_producer(const CUtensorMap* tmQ, const CUten
         for (int t = 0; t < Work::kTiles; ++t)
 #pragma unroll
             for (int h = 0; h < Cfg::kHalves; ++h)
-                tma_load_tile<kStrided>(smem + Cfg::kOffQ + qs * Work::kQStride + t * Cfg::kTileBytes + h * kHalfTileBytes, tmQ,
+                tma_load_tile<kStrided>(smem + Cfg::kOffQ + (qs * 2 + t) * Cfg::kTileBytes + h * kHalfTileBytes, tmQ,
                               &bars->q_full[qs], wk.orders & 15, h * kBoxCols, blk * Work::kRows + t * kBlockQ, head, batch, bh);
         const int n = max(n_a, n_b);
         for (int j = 0; j < n; ++j, ++g) {
             const int st = g & 1;
             const uint32_t ph = (g >> 1) & 1;
-            const int key0 = (kWindow ? span.at(j) : j) * kBlockK;
             ok = mbar_wait(&bars->k_empty[st], ph ^ 1, abort_flag, limit);
             if (!ok) break;
             // `inject` (a test aid, 0 in normal use): the very first K tile is never requested, so the wait for
@@ -175,8 +159,8 @@ __device__ __forceinline__ void fwd_producer(const CUtensorMap* tmQ, const CUten
 #pragma unroll
                 for (int h = 0; h < Cfg::kHalves; ++h)
                     tma_load_tile<kStrided>(smem + Cfg::kOffK + st * Cfg::kTileBytes + h * kHalfTileBytes, tmK,
-                                            &bars->k_full[st], (wk.orders >> 4) & 15, h * kBoxCols, key0, kv_head,
-                                            batch, kv_bh);
+                                            &bars->k_full[st], (wk.orders >> 4) & 15, h * kBoxCols, j * kBlockK, head,
+                                            batch, bh);
             }
             ok = mbar_wait(&bars->v_empty[st], ph ^ 1, abort_flag, limit);
             if (!ok) break;
@@ -185,7 +169,7 @@ __device__ __forceinline__ void fwd_producer(const CUtensorMap* tmQ, const CUten
 #pragma unroll
             for (int h = 0; h < Cfg::kHalves; ++h)
                 tma_load_tile<kStrided>(smem + Cfg::kOffV + st * Cfg::kTileBytes + h * kHalfTileBytes, tmV, &bars->v_full[st],
-                              (wk.orders >> 8) & 15, h * kBoxCols, key0, kv_head, batch, kv_bh);
+                              (wk.orders >> 8) & 15, h * kBoxCols, j * kBlockK, head, batch, bh);
         }
         if (!ok) break;
         // All loads of this item are on their way (the other roles are about two key tiles behind): only now
@@ -710,7 +694,7 @@ __device__ __forceinline__ void fwd_mma_single(uint8_t* smem, FwdBars* bars, uin
     constexpr int kNotPeeked = -3;
     int peeked = kNotPeeked;    // the next item's number, if it was looked at from inside the current item
     bool first_queued = false;  // ... and its first Q K^T was queued from there
-    auto q_desc_of = [&](int stage) { return umma_desc_lo(smem_u32(smem + Cfg::kOffQ + stage * Work::kQStride), 16); };
+    auto q_desc_of = [&](int stage) { return umma_desc_lo(smem_u32(smem + Cfg::kOffQ + stage * 2 * Cfg::kTileBytes), 16); };
     for (;;) {
         const int item = (peeked != kNotPeeked) ? peeked : bars->ring.take(w, lane, abort_flag, limit);
         peeked = kNotPeeked;
@@ -720,23 +704,23 @@ __device__ __forceinline__ void fwd_mma_single(uint8_t* smem, FwdBars* bars, uin
         }
         int blk, bh, n, n_b;
         wk.get(item, &blk, &bh, &n, &n_b);
-        const int qs = w % Work::kQStages;
+        const int qs = w % Cfg::kQStages;
         const uint32_t q_k = q_desc_of(qs);
         if (!first_queued) {
-            ok = mbar_wait(&bars->q_full[qs], (w / Work::kQStages) & 1, abort_flag, limit);
+            ok = mbar_wait(&bars->q_full[qs], (w / Cfg::kQStages) & 1, abort_flag, limit);
             if (ok) issue_qk(g, q_k);
         }
         first_queued = false;
         if (ok && n > 1) issue_qk(g + 1, q_k);
         for (int j = 0; j < n && ok; ++j, ++g) {
             const int st = g & 1;
-            if (Work::kQStages > 1 && j + 1 == n && bars->ring.published(w + 1)) {
+            if (Cfg::kQStages > 1 && j + 1 == n && bars->ring.published(w + 1)) {
                 // Last key tile: the first Q K^T of the next item, if its Q and K have landed, so that neither softmax group
                 // waits at the item boundary.
                 peeked = bars->ring.take(w + 1, lane, abort_flag, limit);
                 if (peeked >= 0) {
-                    const int qs2 = (w + 1) % Work::kQStages;
-                    const bool there = mbar_test(&bars->q_full[qs2], ((w + 1) / Work::kQStages) & 1) &&
+                    const int qs2 = (w + 1) % Cfg::kQStages;
+                    const bool there = mbar_test(&bars->q_full[qs2], ((w + 1) / Cfg::kQStages) & 1) &&
                                        mbar_test(&bars->k_full[st ^ 1], ((g + 1) >> 1) & 1);
                     if (__all_sync(0xffffffffu, there)) {
                         issue_qk(g + 1, q_desc_of(qs2));
@@ -782,11 +766,10 @@ __device__ __forceinline__ void fwd_mma_single(uint8_t* smem, FwdBars* bars, uin
     }
 }
 
-// `rest`, `so`: kWindow alone, null or where the part of O goes that rounding takes from it.
-template <int D, bool kCausal, bool kStrided, bool kWindow, typename Work>
+template <int D, bool kCausal, bool kStrided, typename Work>
 __device__ __forceinline__ void fwd_softmax_single(uint8_t* smem, FwdBars* bars, uint32_t tmem_base, const CUtensorMap* tmO,
-                                                   float* __restrict__ LSE, uint16_t* __restrict__ rest, const TensorStrides& so,
-                                                   float scale, const Work& wk, int t, int swarp, int lane, long long limit) {
+                                                   float* __restrict__ LSE, float scale, const Work& wk, int t, int swarp,
+                                                   int lane, long long limit) {
     using Cfg = FwdCfg<D>;
     volatile int* abort_flag = &bars->abort_flag;
     const uint32_t lane_base = 32u * (swarp & 3);
@@ -796,7 +779,7 @@ __device__ __forceinline__ void fwd_softmax_single(uint8_t* smem, FwdBars* bars,
     const uint32_t t_o_half = tmem_addr(tmem_base, lane_base, Cfg::kColO + D / 2 * t);
     // [item & 1][group][row], in the unused Q buffer of tile B.  Two items' worth: a group may be through the tiles of
     // the next item (if there are no more than two) before the other has read the sums of this one.
-    float2* sums = reinterpret_cast<float2*>(smem + Work::kOffSums);
+    float2* sums = reinterpret_cast<float2*>(smem + Cfg::kOffQ + Cfg::kTileBytes);
     const float c = scale * kLog2e;
     const uint64_t c2 = f32x2_pack(c, c);
     const int T = wk.T;
@@ -812,7 +795,6 @@ __device__ __forceinline__ void fwd_softmax_single(uint8_t* smem, FwdBars* bars,
         int blk, bh, n, n_b;
         wk.get(item, &blk, &bh, &n, &n_b);
         const int row = blk * kBlockQ + row_local;
-        const KeySpan span = kWindow ? wk.span(blk) : KeySpan{0, 0, 0};
         float m_ref = -INFINITY, l = 0.f;  // -inf while the half has had no key that the row keeps
         for (int j = 0; j < n; ++j, ++cnt) {
             const int buf = cnt & 1;
@@ -824,23 +806,13 @@ __device__ __forceinline__ void fwd_softmax_single(uint8_t* smem, FwdBars* bars,
             tmem_ld_x32(t_s, sr);
             tmem_ld_x32(t_s + 32, sr + 32);
             tmem_wait_ld();
-            if constexpr (kWindow) {  // (rows past the end of the sequence keep what the last one does)
-                const int key0 = span.at(j) * kBlockK + 64 * t, last = min(blk * kBlockQ + kBlockQ, T) - 1;
-                if (any_dropped(wk.win, blk * kBlockQ, last, key0)) {
-                    const uint64_t kept = kept_keys(wk.win, min(row, T - 1), key0);
+            const bool diag = kCausal && (j == blk);
+            const int keys_left = T - j * kBlockK;
+            if (diag || keys_left < kBlockK) {
+                const int lim = (diag ? min(row_local, keys_left - 1) : keys_left - 1) - 64 * t;
 #pragma unroll
-                    for (int i = 0; i < 64; ++i)
-                        if (!(static_cast<uint32_t>(kept >> (i & 32)) >> (i & 31) & 1u)) sr[i] = 0xff800000u;  // -inf
-                }
-            } else {
-                const bool diag = kCausal && (j == blk);
-                const int keys_left = T - j * kBlockK;
-                if (diag || keys_left < kBlockK) {
-                    const int lim = (diag ? min(row_local, keys_left - 1) : keys_left - 1) - 64 * t;
-#pragma unroll
-                    for (int i = 0; i < 64; ++i)
-                        if (i > lim) sr[i] = 0xff800000u;  // -inf
-                }
+                for (int i = 0; i < 64; ++i)
+                    if (i > lim) sr[i] = 0xff800000u;  // -inf
             }
             float mx0 = fmaxf(__uint_as_float(sr[0]), __uint_as_float(sr[1]));
             float mx1 = fmaxf(__uint_as_float(sr[2]), __uint_as_float(sr[3]));
@@ -912,8 +884,8 @@ __device__ __forceinline__ void fwd_softmax_single(uint8_t* smem, FwdBars* bars,
         s_w[t * kBlockQ + row_local] = make_float2(m_ref, l);
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars->sums_ready);
-        const int qs = w % Work::kQStages;
-        uint8_t* stage = smem + Cfg::kOffQ + qs * Work::kQStride;  // no longer read: every Q K^T has completed
+        const int qs = w % Cfg::kQStages;
+        uint8_t* stage = smem + Cfg::kOffQ + qs * 2 * Cfg::kTileBytes;  // no longer read: every Q K^T has completed
         ok = mbar_wait(&bars->sums_ready, w & 1, abort_flag, limit);
         // Not pv_done: of the tile before the last, P V may be outstanding still (S runs two tiles ahead, and the other group
         // may be a tile behind), and a wait two phases on would pass at once.
@@ -921,7 +893,7 @@ __device__ __forceinline__ void fwd_softmax_single(uint8_t* smem, FwdBars* bars,
         if (!ok) break;
         tc_fence_after();
         const float2 s0 = s_w[row_local], s1 = s_w[kBlockQ + row_local];
-        const float m = fmaxf(s0.x, s1.x);  // finite: every row keeps key 0 (with the window itself), which is in one of the halves
+        const float m = fmaxf(s0.x, s1.x);  // finite: key 0 is in the first half and every row keeps it
         const float f0 = ex2_approx((s0.x - m) * c), f1 = ex2_approx((s1.x - m) * c);  // 2^-inf = 0
         l = s0.y * f0 + s1.y * f1;
         const float i0 = f0 / l, i1 = f1 / l;
@@ -937,21 +909,11 @@ __device__ __forceinline__ void fwd_softmax_single(uint8_t* smem, FwdBars* bars,
             for (int x = 0; x < 4; ++x) {
                 const int ch = (col % 64) / 8 + x;  // 16-byte chunk of the 128-byte swizzled row
                 uint32_t v[4];
-                uint32_t r[4];
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const float o0 = fmaf(__uint_as_float(a[8 * x + 2 * y]), i0, __uint_as_float(b[8 * x + 2 * y]) * i1);
-                    const float o1 = fmaf(__uint_as_float(a[8 * x + 2 * y + 1]), i0, __uint_as_float(b[8 * x + 2 * y + 1]) * i1);
-                    v[y] = pack_bf16x2(o0, o1);
-                    if constexpr (kWindow)
-                        r[y] = pack_bf16x2(o0 - __uint_as_float(v[y] << 16), o1 - __uint_as_float(v[y] & 0xffff0000u));
-                }
+                for (int y = 0; y < 4; ++y)
+                    v[y] = pack_bf16x2(fmaf(__uint_as_float(a[8 * x + 2 * y]), i0, __uint_as_float(b[8 * x + 2 * y]) * i1),
+                                       fmaf(__uint_as_float(a[8 * x + 2 * y + 1]), i0, __uint_as_float(b[8 * x + 2 * y + 1]) * i1));
                 *reinterpret_cast<uint4*>(row_ptr + ((ch ^ (row_local & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
-                if constexpr (kWindow) {
-                    if (rest != nullptr && row < T)
-                        *reinterpret_cast<uint4*>(rest + (bh / wk.H) * so.b + (bh % wk.H) * so.h + row * so.t + col + 8 * x) =
-                            make_uint4(r[0], r[1], r[2], r[3]);
-                }
             }
         }
         tc_fence_before();
@@ -971,13 +933,13 @@ __device__ __forceinline__ void fwd_softmax_single(uint8_t* smem, FwdBars* bars,
                     tma_store_tile<kStrided>(tmO, stage + h * kHalfTileBytes, (wk.orders >> 12) & 15, h * kBoxCols,
                                              blk * kBlockQ, kStrided ? bh % wk.H : 0, kStrided ? bh / wk.H : 0, bh);
                 bulk_commit_group();
-                if (Work::kQStages == 1) {  // the next item's Q tile needs this very buffer
+                if (Cfg::kQStages == 1) {  // the next item's Q tile needs this very buffer
                     bulk_wait_group_read<0>();
                     mbar_arrive(&bars->q_empty[qs]);
                 }
             }
         }
-        if (Work::kQStages > 1) pending_qs = qs;  // handed back after the next item's first tile, as with pairs
+        if (Cfg::kQStages > 1) pending_qs = qs;  // handed back after the next item's first tile, as with pairs
         ok = __all_sync(0xffffffffu, leader_ok);
         if (!ok) break;
         ++w;
@@ -985,21 +947,19 @@ __device__ __forceinline__ void fwd_softmax_single(uint8_t* smem, FwdBars* bars,
     if (leader) bulk_wait_group<0>();  // O must be complete before the kernel ends
 }
 
-template <int D, bool kCausal, bool kStrided, bool kSingle, bool kOwn, bool kWindow>
+template <int D, bool kCausal, bool kStrided, bool kSingle, bool kOwn>
 __global__ void __launch_bounds__(kFwdThreads, 1)
 attn_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                 const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmO,
                 float* __restrict__ LSE, int T, int BH, int H, uint32_t orders, int n_blocks, int chunk, float scale,
-                long long limit, int inject, int* __restrict__ dev_status, const Window win, uint16_t* __restrict__ rest,
-                const TensorStrides so) {
-    static_assert(!kWindow || (kSingle && kCausal && !kOwn), "the window has single tiles only");
+                long long limit, int inject, int* __restrict__ dev_status) {
     using Cfg = FwdCfg<D>;
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     FwdBars* bars = reinterpret_cast<FwdBars*>(smem + Cfg::kOffBar);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    using Work = FwdWork<D, kSingle, kOwn, kWindow>;
-    const Work wk{n_blocks * BH, BH, n_blocks, (T + kBlockK - 1) / kBlockK, T, H, chunk, orders, kCausal, win};
+    using Work = FwdWork<D, kSingle, kOwn>;
+    const Work wk{n_blocks * BH, BH, n_blocks, (T + kBlockK - 1) / kBlockK, T, H, chunk, orders, kCausal};
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < 2; ++s) {
@@ -1045,13 +1005,11 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         {
             wk.get(blockIdx.x, &blk, &bh, &n_a, &n_b);
             const int head = kStrided ? bh % wk.H : 0, batch = kStrided ? bh / wk.H : 0;
-            const int kv_head = kWindow ? head / wk.win.group : head, kv_bh = kWindow ? bh / wk.win.group : bh;
-            const int key0 = kWindow ? wk.span(blk).at(0) * kBlockK : 0;
 #pragma unroll
             for (int h = 0; h < Cfg::kHalves; ++h) {
-                tma_prefetch_tile<kStrided>(&tmK, (wk.orders >> 4) & 15, h * kBoxCols, key0, kv_head, batch, kv_bh);
+                tma_prefetch_tile<kStrided>(&tmK, (wk.orders >> 4) & 15, h * kBoxCols, 0, head, batch, bh);
                 tma_prefetch_tile<kStrided>(&tmQ, wk.orders & 15, h * kBoxCols, blk * Work::kRows, head, batch, bh);
-                tma_prefetch_tile<kStrided>(&tmV, (wk.orders >> 8) & 15, h * kBoxCols, key0, kv_head, batch, kv_bh);
+                tma_prefetch_tile<kStrided>(&tmV, (wk.orders >> 8) & 15, h * kBoxCols, 0, head, batch, bh);
                 if (!kSingle)
                     tma_prefetch_tile<kStrided>(&tmQ, wk.orders & 15, h * kBoxCols, blk * Work::kRows + kBlockQ, head, batch, bh);
             }
@@ -1060,15 +1018,14 @@ attn_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     griddep_wait();  // everything above overlaps the previous kernel of the stream
 
     if (warp == 0) {
-        if (lane == 0) fwd_producer<D, kStrided, kWindow>(&tmQ, &tmK, &tmV, smem, bars, wk, limit, inject);
+        if (lane == 0) fwd_producer<D, kStrided>(&tmQ, &tmK, &tmV, smem, bars, wk, limit, inject);
     } else if (warp == 1) {
         if constexpr (kSingle) fwd_mma_single<D>(smem, bars, tmem_base, wk, limit);
         else fwd_mma<D>(smem, bars, tmem_base, wk, limit);
     } else if (warp >= 4) {
         const int t = (warp - 4) >> 2;
         if constexpr (kSingle)
-            fwd_softmax_single<D, kCausal, kStrided, kWindow>(smem, bars, tmem_base, &tmO, LSE, rest, so, scale, wk, t,
-                                                              (warp - 4) & 3, lane, limit);
+            fwd_softmax_single<D, kCausal, kStrided>(smem, bars, tmem_base, &tmO, LSE, scale, wk, t, (warp - 4) & 3, lane, limit);
         else
             fwd_softmax<D, kCausal, kStrided>(smem, bars, tmem_base, &tmO, LSE, scale, wk, t, (warp - 4) & 3, lane, limit);
     }
@@ -1112,19 +1069,16 @@ cudaError_t launch_one(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUt
     const dim3 grid(static_cast<unsigned>(n_blocks) * BH);  // one CTA per item; those that do not start at once are taken over
     auto go = [&](auto kernel) {
         return launch_overlapped(kernel, grid, dim3(kFwdThreads), FwdCfg<D>::kSmemBytes, stream, tmQ, tmK, tmV, tmO, LSE, s.T,
-                                 BH, s.H, orders, n_blocks, chunk, s.scale, wait_limit, inject, dev_status, Window{}, nullptr,
-                                 TensorStrides{});
+                                 BH, s.H, orders, n_blocks, chunk, s.scale, wait_limit, inject, dev_status);
     };
     if (single)
-        return strided ? go(attn_fwd_kernel<D, kCausal, true, true, false, false>)
-                       : go(attn_fwd_kernel<D, kCausal, false, true, false, false>);
+        return strided ? go(attn_fwd_kernel<D, kCausal, true, true, false>) : go(attn_fwd_kernel<D, kCausal, false, true, false>);
     if constexpr (D == 128) {
         if (static_cast<long long>(n_blocks) * BH > num_sms)
-            return strided ? go(attn_fwd_kernel<D, kCausal, true, false, true, false>)
-                           : go(attn_fwd_kernel<D, kCausal, false, false, true, false>);
+            return strided ? go(attn_fwd_kernel<D, kCausal, true, false, true>)
+                           : go(attn_fwd_kernel<D, kCausal, false, false, true>);
     }
-    return strided ? go(attn_fwd_kernel<D, kCausal, true, false, false, false>)
-                   : go(attn_fwd_kernel<D, kCausal, false, false, false, false>);
+    return strided ? go(attn_fwd_kernel<D, kCausal, true, false, false>) : go(attn_fwd_kernel<D, kCausal, false, false, false>);
 }
 
 template <int D, bool kCausal, bool kStrided>
@@ -1132,13 +1086,10 @@ cudaError_t configure_one() {
     auto set = [](auto kernel) {
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FwdCfg<D>::kSmemBytes);
     };
-    cudaError_t e = set(attn_fwd_kernel<D, kCausal, kStrided, false, false, false>);
-    if (e == cudaSuccess) e = set(attn_fwd_kernel<D, kCausal, kStrided, true, false, false>);
+    cudaError_t e = set(attn_fwd_kernel<D, kCausal, kStrided, false, false>);
+    if (e == cudaSuccess) e = set(attn_fwd_kernel<D, kCausal, kStrided, true, false>);
     if constexpr (D == 128) {
-        if (e == cudaSuccess) e = set(attn_fwd_kernel<D, kCausal, kStrided, false, true, false>);
-    }
-    if constexpr (kCausal) {
-        if (e == cudaSuccess) e = set(attn_fwd_kernel<D, true, kStrided, true, false, true>);
+        if (e == cudaSuccess) e = set(attn_fwd_kernel<D, kCausal, kStrided, false, true>);
     }
     return e;
 }
@@ -1164,22 +1115,6 @@ cudaError_t launch_attn_fwd(const CUtensorMap& tmQ, const CUtensorMap& tmK, cons
     }
     return s.causal ? launch_one<128, true>(tmQ, tmK, tmV, tmO, strided, orders, LSE, s, num_sms, wait_limit, inject, dev_status, stream)
                     : launch_one<128, false>(tmQ, tmK, tmV, tmO, strided, orders, LSE, s, num_sms, wait_limit, inject, dev_status, stream);
-}
-
-cudaError_t launch_window_fwd(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmO,
-                              bool strided, uint32_t orders, float* LSE, __nv_bfloat16* rest, const TensorStrides& so,
-                              const AttnShape& s, const Window& win, int num_sms, int* dev_status, cudaStream_t stream) {
-    const int BH = s.B * s.H, n_blocks = (s.T + kBlockQ - 1) / kBlockQ;
-    const dim3 grid(static_cast<unsigned>(n_blocks) * BH);  // one CTA per item; those that do not start at once are taken over
-    auto go = [&](auto kernel, int smem) {
-        return launch_overlapped(kernel, grid, dim3(kFwdThreads), smem, stream, tmQ, tmK, tmV, tmO, LSE, s.T, BH, s.H, orders,
-                                 n_blocks, BH, s.scale, kWaitLimitCycles, 0, dev_status, win, reinterpret_cast<uint16_t*>(rest), so);
-    };
-    if (s.D == 64)
-        return strided ? go(attn_fwd_kernel<64, true, true, true, false, true>, FwdCfg<64>::kSmemBytes)
-                       : go(attn_fwd_kernel<64, true, false, true, false, true>, FwdCfg<64>::kSmemBytes);
-    return strided ? go(attn_fwd_kernel<128, true, true, true, false, true>, FwdCfg<128>::kSmemBytes)
-                   : go(attn_fwd_kernel<128, true, false, true, false, true>, FwdCfg<128>::kSmemBytes);
 }
 
 }  // namespace nova

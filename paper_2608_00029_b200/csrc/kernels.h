@@ -109,10 +109,6 @@ inline cudaError_t launch_overlapped(void (*kernel)(KArgs...), dim3 grid, dim3 b
 cudaError_t launch_attn_fwd(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
                             const CUtensorMap& tmO, bool strided, uint32_t orders, float* LSE, const AttnShape& s,
                             int num_sms, long long wait_limit, int inject, int* dev_status, cudaStream_t stream);
-// With the window: K and V maps have B * H / win.group heads; `rest` null or a tensor with O's strides `so`.
-cudaError_t launch_window_fwd(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmO,
-                              bool strided, uint32_t orders, float* LSE, __nv_bfloat16* rest, const TensorStrides& so,
-                              const AttnShape& s, const Window& win, int num_sms, int* dev_status, cudaStream_t stream);
 cudaError_t configure_attn_fwd();
 
 // `rest`: what rounding took from O, with its strides, or null.
@@ -133,7 +129,7 @@ cudaError_t launch_attn_dq(const CUtensorMap& tmQ, const CUtensorMap& tmK, const
                            const CUtensorMap& tmdO, const CUtensorMap& tmdQ, bool strided, uint32_t orders,
                            const float* LSE, const float* Delta, const AttnShape& s, int num_sms, int* dev_status,
                            cudaStream_t stream);
-// With the window (D = 128), as in the forward.
+// With the window (D = 128): K and V maps have B * H / win.group heads.
 cudaError_t launch_window_dq(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
                              const CUtensorMap& tmdQ, bool strided, uint32_t orders, const float* LSE, const float* Delta,
                              const AttnShape& s, const Window& win, int num_sms, int* dev_status, cudaStream_t stream);
@@ -242,6 +238,9 @@ bool lmhead_rows_plan(int M, int N, int num_sms, int* ctas, int* tile_h, int* m_
 cudaError_t launch_lmhead_rows(const CUtensorMap& tmX, const CUtensorMap& tmW, const int* targets, void* logits,
                                float* lse, float* loss, int M, int N, int K, int ctas, int tile_h, int m_pad,
                                void* workspace, float* tgt_logit, int* dev_status, cudaStream_t stream);
+
+// The forward of the attention with a window (ops/window_fwd.cu).
+cudaError_t configure_window_fwd();
 
 // Clears `bytes` (a multiple of 16) at the 16-byte aligned `ptr`.
 cudaError_t launch_zero(void* ptr, size_t bytes, int num_sms, cudaStream_t stream);

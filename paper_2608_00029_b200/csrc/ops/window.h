@@ -1,9 +1,14 @@
-// The attention with a sliding window and sinks: its single-token form between the entry points and the kernels.  Not installed.
+// The attention with a sliding window and sinks between the entry points and the kernels.  Not installed.
 #pragma once
 
 #include "../kernels.h"
 
 namespace nova {
+
+// K and V maps have B * H / win.group heads and boxes of kKeyStep rows; O and `rest` (which may be null) have strides `so`.
+cudaError_t launch_window_fwd(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, bool strided, uint32_t orders,
+                              __nv_bfloat16* O, __nv_bfloat16* rest, float* LSE, const TensorStrides& so, const AttnShape& s,
+                              const Window& win, int* dev_status, cudaStream_t stream);
 
 struct DecodeArgs {
     const uint16_t *q, *k, *v;

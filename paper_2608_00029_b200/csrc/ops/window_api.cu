@@ -49,16 +49,15 @@ int nova_window_fwd(const void* Q, const void* K, const void* V, void* O, void* 
     if (int rc = device_state(&st)) return rc;
     const AttnShape s{B, H, T, D, 1, scale}, s_kv{B, H_kv, T, D, 1, scale};
     const Window win{std::min(window, T), std::min(sinks, T), H / H_kv};
-    CUtensorMap tmQ, tmK, tmV, tmO;
-    uint32_t oq, ok, ov, oo;
-    const bool strided = !(merges(s, sq) && merges(s_kv, sk) && merges(s_kv, sv) && merges(s, so));
+    CUtensorMap tmQ, tmK, tmV;
+    uint32_t oq, ok, ov;
+    const bool strided = !(merges(s, sq) && merges(s_kv, sk) && merges(s_kv, sv));
     if (int rc = get_bf16_map(Q, s, sq, strided, &tmQ, &oq)) return rc;
-    if (int rc = get_bf16_map(K, s_kv, sk, strided, &tmK, &ok)) return rc;
-    if (int rc = get_bf16_map(V, s_kv, sv, strided, &tmV, &ov)) return rc;
-    if (int rc = get_bf16_map(O, s, so, strided, &tmO, &oo)) return rc;
-    const uint32_t orders = oq | (ok << 4) | (ov << 8) | (oo << 12);
-    const cudaError_t e = launch_window_fwd(tmQ, tmK, tmV, tmO, strided, orders, LSE, static_cast<__nv_bfloat16*>(O_rest), so, s, win,
-                                            st->num_sms, st->dev_status, static_cast<cudaStream_t>(stream));
+    if (int rc = get_bf16_map(K, s_kv, sk, strided, &tmK, &ok, kKeyStep)) return rc;
+    if (int rc = get_bf16_map(V, s_kv, sv, strided, &tmV, &ov, kKeyStep)) return rc;
+    const uint32_t orders = oq | (ok << 4) | (ov << 8);
+    const cudaError_t e = launch_window_fwd(tmQ, tmK, tmV, strided, orders, static_cast<__nv_bfloat16*>(O), static_cast<__nv_bfloat16*>(O_rest),
+                                            LSE, so, s, win, st->dev_status, static_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? NOVA_ATTN_OK : record_cuda_error(e);
 }
 
