@@ -57,6 +57,11 @@ __device__ __forceinline__ uint64_t bits_below(int n) { return n <= 0 ? 0ull : n
 __device__ __forceinline__ uint64_t kept_keys(const Window& w, int row, int k0) {
     return bits_below(row + 1 - k0) & (~bits_below(row + 1 - w.window - k0) | bits_below(w.sinks - k0));
 }
+// The same of 32.
+__device__ __forceinline__ uint32_t bits_below_32(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
+__device__ __forceinline__ uint32_t kept_keys_32(const Window& w, int row, int k0) {
+    return bits_below_32(row + 1 - k0) & (~bits_below_32(row + 1 - w.window - k0) | bits_below_32(w.sinks - k0));
+}
 // Is there anything among the 64 keys from k0 on that one of the queries q0 .. q1 does not keep?
 __device__ __forceinline__ bool any_dropped(const Window& w, int q0, int q1, int k0) {
     return k0 + 63 > q0 || (q1 - k0 >= w.window && k0 + 64 > w.sinks);

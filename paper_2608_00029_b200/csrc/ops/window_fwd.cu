@@ -293,42 +293,37 @@ __device__ __forceinline__ void softmax(Bars* bars, uint32_t tmem_base, uint16_t
         for (int j = 0; j < span.n; ++j, ++g) {
             const int buf = g & 1, key0 = span.at(j) * kStep;
             const uint32_t t_s = tmem_addr(tmem_base, lane_base, C::kColS + kStep * buf);
-            // Halves of 32 keys: does any of the warp's rows keep any of it, and all of them all of it?  Both the same in every lane.
-            bool need[2], whole = true;
+            // Halves of 32 keys: does any of the warp's rows keep any of it, and all of them all of it?  The same in every lane.
+            bool need[2], whole[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int k0 = key0 + 32 * h;
                 need[h] = k0 <= last && (k0 + 31 > row0 - wk.win.window || k0 < wk.win.sinks);
-                whole = whole && k0 + 31 <= row0 && (k0 > row0 + 31 - wk.win.window || k0 + 31 < wk.win.sinks);
+                whole[h] = k0 + 31 <= row0 && (k0 > row0 + 31 - wk.win.window || k0 + 31 < wk.win.sinks);
             }
             ok = mbar_wait(&bars->s_full[buf], (g >> 1) & 1, abort_flag);
             if (!ok) break;
             tc_fence_after();
             uint32_t sr[kStep];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                if (need[h]) {
-                    tmem_ld_x32(t_s + 32 * h, sr + 32 * h);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) sr[32 * h + i] = 0xff800000u;  // -inf
-                }
-            }
+            for (int h = 0; h < 2; ++h)
+                if (need[h]) tmem_ld_x32(t_s + 32 * h, sr + 32 * h);
             tmem_wait_ld();
-            if (!whole) {
-                const uint64_t kept = kept_keys(wk.win, kept_row, key0);
+            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int i = 0; i < kStep; ++i)
-                    if (!(static_cast<uint32_t>(kept >> (i & 32)) >> (i & 31) & 1u)) sr[i] = 0xff800000u;
-            }
-            float mx0 = fmaxf(__uint_as_float(sr[0]), __uint_as_float(sr[1]));
-            float mx1 = fmaxf(__uint_as_float(sr[2]), __uint_as_float(sr[3]));
+            for (int h = 0; h < 2; ++h) {
+                if (!need[h]) continue;
+                if (!whole[h]) {
+                    const uint32_t kept = kept_keys_32(wk.win, kept_row, key0 + 32 * h);
 #pragma unroll
-            for (int i = 4; i < kStep; i += 4) {
-                mx0 = fmax3(mx0, __uint_as_float(sr[i + 0]), __uint_as_float(sr[i + 1]));
-                mx1 = fmax3(mx1, __uint_as_float(sr[i + 2]), __uint_as_float(sr[i + 3]));
+                    for (int i = 0; i < 32; ++i)
+                        if (!(kept >> i & 1u)) sr[32 * h + i] = 0xff800000u;  // -inf
+                }
+#pragma unroll
+                for (int i = 0; i < 32; i += 2)
+                    mx[i / 2 % 4] = fmax3(mx[i / 2 % 4], __uint_as_float(sr[32 * h + i]), __uint_as_float(sr[32 * h + i + 1]));
             }
-            const float m_new = fmaxf(m_ref, fmaxf(mx0, mx1));
+            const float m_new = fmaxf(m_ref, fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])));
             if (j == 0) {
                 m_ref = m_new;
             } else if (__any_sync(0xffffffffu, (m_new - m_ref) * c > kRescaleThreshold)) {  // (-inf against -inf: no)
@@ -354,7 +349,7 @@ __device__ __forceinline__ void softmax(Bars* bars, uint32_t tmem_base, uint16_t
             const float mc_near = m_ref * c, mc_up = __fmul_ru(m_ref, c);
             const float mc = m_ref == -INFINITY ? 0.f : fabsf(mc_near) > 1e9f ? mc_up : mc_near;
             const uint64_t nmc2 = f32x2_pack(-mc, -mc);
-            uint64_t acc0 = 0, acc1 = 0;
+            uint64_t acc[4] = {0, 0, 0, 0};
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint32_t pk[16];
@@ -366,10 +361,10 @@ __device__ __forceinline__ void softmax(Bars* bars, uint32_t tmem_base, uint16_t
                         f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(s[0]), __uint_as_float(s[1])), c2, nmc2), x0, x1);
                         f32x2_unpack(f32x2_fma(f32x2_pack(__uint_as_float(s[2]), __uint_as_float(s[3])), c2, nmc2), x2, x3);
                         const float p0 = ex2_approx(x0), p1 = ex2_approx(x1), p2 = ex2_approx(x2), p3 = ex2_approx(x3);
-                        acc0 = f32x2_add(acc0, f32x2_pack(p0, p1));
-                        acc1 = f32x2_add(acc1, f32x2_pack(p2, p3));
-                        pk[i / 2] = pack_bf16x2(p0, p1);
-                        pk[i / 2 + 1] = pack_bf16x2(p2, p3);
+                        acc[i / 2 % 4] = f32x2_add(acc[i / 2 % 4], f32x2_pack(p0, p1));
+                        acc[i / 2 % 4 + 1] = f32x2_add(acc[i / 2 % 4 + 1], f32x2_pack(p2, p3));
+                        pk[i / 2] = pack_bf16x2_int(p0, p1);
+                        pk[i / 2 + 1] = pack_bf16x2_int(p2, p3);
                     }
                 } else {
 #pragma unroll
@@ -378,8 +373,8 @@ __device__ __forceinline__ void softmax(Bars* bars, uint32_t tmem_base, uint16_t
                 tmem_st_x16(t_s + 16 * h, pk);
             }
             float a0, a1, a2, a3;
-            f32x2_unpack(acc0, a0, a1);
-            f32x2_unpack(acc1, a2, a3);
+            f32x2_unpack(f32x2_add(acc[0], acc[2]), a0, a1);
+            f32x2_unpack(f32x2_add(acc[1], acc[3]), a2, a3);
             l += (a0 + a1) + (a2 + a3);
             tmem_wait_st();
             tc_fence_before();
