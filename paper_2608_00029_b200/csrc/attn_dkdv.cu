@@ -63,27 +63,46 @@ struct KvBars {
 };
 static_assert(sizeof(KvBars) <= 512, "barrier block");
 
-// Work items: 128-key tiles; heads in chunks, heaviest tiles first within a chunk.  kWindow: the heads are those of K and V, and an
-// item has the steps of all query heads that share its head, one after another.
+// Work items: 128-key tiles; heads in chunks, heaviest tiles first within a chunk.  kWindow: the heads are those of K and V, and the
+// list of a tile has the steps of all query heads that share its head, one after another; an item is a part of it (KvParts).
 template <bool kWindow>
 struct KvWork {
     int BH, n_tiles, chunk, T, H;
     uint32_t orders;  // coordinate orders of the Q, K, V, dO, dK, dV tensor maps, four bits each
     bool causal;
     Window win;
-    // Steps of one query head in an item of n.
+    KvParts parts;
+    // First step of item `idx` in its tile's list, and its slot of the workspace (-1: none).
+    __device__ __forceinline__ int offset(int idx) const {
+        if (!kWindow || kv_parts_of(parts, BH, idx) == 1) return 0;
+        const KvItem it = kv_item(parts, BH, idx);
+        int first, n;
+        kv_part(win.group * query_steps(win, it.kt * kBlockK, kBlockK, T, kStep), it.part, it.parts, &first, &n);
+        return first;
+    }
+    __device__ __forceinline__ int slot(int idx) const { return kWindow && kv_parts_of(parts, BH, idx) > 1 ? kv_item(parts, BH, idx).slot : -1; }
+    // Steps of one query head in the list of a tile (of n steps without the window).
     __device__ __forceinline__ int per_head(int kt, int n) const {
         return kWindow ? query_steps(win, kt * kBlockK, kBlockK, T, kStep) : n;
     }
     // Key tile, head, first step and number of steps of item `idx`.
     __device__ __forceinline__ void get(int idx, int* kt, int* bh, int* s0, int* n) const {
+        if constexpr (kWindow) {
+            const KvItem it = kv_item(parts, BH, idx);
+            *kt = it.kt;
+            *bh = it.bh;
+            *s0 = it.kt * (kBlockK / kStep);
+            int first;
+            kv_part(win.group * query_steps(win, it.kt * kBlockK, kBlockK, T, kStep), it.part, it.parts, &first, n);
+            return;
+        }
         const int per_chunk = chunk * n_tiles;
         const int ck = idx / per_chunk, in = idx - ck * per_chunk;
         const int heads = min(chunk, BH - ck * chunk);
         *kt = in / heads;
         *bh = ck * chunk + in - *kt * heads;
         *s0 = causal ? *kt * (kBlockK / kStep) : 0;
-        *n = kWindow ? win.group * query_steps(win, *kt * kBlockK, kBlockK, T, kStep) : (T + kStep - 1) / kStep - *s0;
+        *n = (T + kStep - 1) / kStep - *s0;
     }
 };
 
@@ -114,7 +133,9 @@ __device__ __forceinline__ void kv_producer(const CUtensorMap* tmQ, const CUtens
             tma_load_tile<kStrided>(smem + kOffK + ks * kTileBytes + h * kHalfTileBytes, tmK, &bars->k_full[ks],
                                     (wk.orders >> 4) & 15, h * kBoxCols, kt * kBlockK, head, batch, bh);
         const int per = wk.per_head(kt, n);
-        int q_head = kWindow ? head * wk.win.group : head, q_bh = kWindow ? bh * wk.win.group : bh, sh = 0;
+        const int off = wk.offset(item), first = kWindow ? off / per : 0;  // the item's first query head of those that share
+        int q_head = kWindow ? head * wk.win.group + first : head, q_bh = kWindow ? bh * wk.win.group + first : bh;
+        int sh = off - first * per;
         for (int s = 0; s < n; ++s) {
             ok = mbar_wait(&bars->q_empty[st], ph ^ 1, abort_flag);
             if (!ok) break;
@@ -332,7 +353,8 @@ __device__ __forceinline__ void kv_row_loader(KvBars* bars, float* row_buf, cons
         int kt, bh, s0, n;
         wk.get(item, &kt, &bh, &s0, &n);
         const int per = wk.per_head(kt, n), last = kWindow ? (bh + 1) * wk.win.group - 1 : bh;
-        int q_bh = kWindow ? bh * wk.win.group : bh, sh = 0;
+        const int off = wk.offset(item), first = kWindow ? off / per : 0;
+        int q_bh = kWindow ? bh * wk.win.group + first : bh, sh = off - first * per;
         for (int s = 0; s < n; s += kDeep) {
             float l[kDeep][2], d[kDeep][2];
 #pragma unroll
@@ -394,7 +416,8 @@ __device__ __forceinline__ void kv_compute(const uint8_t* smem, KvBars* bars, ui
         wk.get(item, &kt, &bh, &s0, &n);
         const int key = kt * kBlockK + r;
         const int per = wk.per_head(kt, n);
-        int sh = (g ^ grp) & 1;  // the step in its query head
+        int sh = 0;  // the step in its query head
+        if constexpr (kWindow) sh = (wk.offset(item) + ((g ^ grp) & 1)) % per;
         for (int s = (g ^ grp) & 1; s < n; s += 2, sh += 2) {
             if constexpr (kWindow)
                 while (sh >= per) sh -= per;
@@ -476,12 +499,14 @@ __device__ __forceinline__ void kv_stage_row(uint8_t* stage, int r, const uint32
 // buffer and out with TMA stores, while the compute warps are in the next item.
 template <bool kStrided, bool kWindow>
 __device__ __forceinline__ void kv_write_out(uint8_t* smem, KvBars* bars, uint32_t tmem_base, const CUtensorMap* tmdK,
-                                             const CUtensorMap* tmdV, float scale, const KvWork<kWindow>& wk, int owarp, int lane) {
+                                             const CUtensorMap* tmdV, float* __restrict__ partial, float scale,
+                                             const KvWork<kWindow>& wk, int owarp, int lane) {
     volatile int* abort_flag = &bars->abort_flag;
     const uint32_t lane_base = 32u * owarp;
     const int r = lane_base + lane;
     const bool leader = (owarp == 0 && lane == 0);
     bool ok = true;
+    int whole = 0;  // kWindow: items whose dV and dK have gone out as bf16
     for (int w = 0;; ++w) {
         const int item = bars->ring.take(w, lane, abort_flag, kWaitLimitCycles);
         if (item < 0) break;
@@ -491,6 +516,29 @@ __device__ __forceinline__ void kv_write_out(uint8_t* smem, KvBars* bars, uint32
         ok = mbar_wait(&bars->dkv_full, w & 1, abort_flag);
         if (!ok) break;
         tc_fence_after();
+        if constexpr (kWindow) {
+            const int slot = wk.slot(item);
+            if (slot >= 0) {  // a part of a tile: the sums as they are, rows past the end of the sequence among them
+                float* const to = partial + (static_cast<size_t>(slot) * 2 * kBlockK + r) * D;
+#pragma unroll
+                for (int cb = 0; cb < 2 * D; cb += 32) {
+                    uint32_t a[32];
+                    tmem_ld_x32(tmem_addr(tmem_base, lane_base, cb < D ? kColdV + cb : kColdK + cb - D), a);
+                    tmem_wait_ld();
+                    float4* const p = reinterpret_cast<float4*>(to + (cb < D ? cb : kBlockK * D + cb - D));
+#pragma unroll
+                    for (int x = 0; x < 8; ++x)
+                        p[x] = make_float4(__uint_as_float(a[4 * x]), __uint_as_float(a[4 * x + 1]), __uint_as_float(a[4 * x + 2]),
+                                           __uint_as_float(a[4 * x + 3]));
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars->dkv_free);
+                if (leader) mbar_arrive(&bars->k_empty[ks]);
+                __syncwarp();
+                continue;
+            }
+        }
         // Both go through the item's K buffer, dV first; dK waits in registers (64 of packed bf16) meanwhile, so that the
         // accumulators are free for the next item at once.
         const int hh = kStrided ? bh % wk.H : 0, bb = kStrided ? bh / wk.H : 0;
@@ -532,7 +580,8 @@ __device__ __forceinline__ void kv_write_out(uint8_t* smem, KvBars* bars, uint32
             }
         }
         ok = __all_sync(0xffffffffu, leader_ok);
-        if (ok) ok = mbar_wait(&bars->stage_free, w & 1, abort_flag);
+        if (ok) ok = mbar_wait(&bars->stage_free, (kWindow ? whole : w) & 1, abort_flag);
+        if constexpr (kWindow) ++whole;
         if (!ok) break;
         kv_stage_row(stage, r, pk[1]);
         fence_proxy_async_smem();
@@ -562,7 +611,8 @@ attn_dkdv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                  const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmdO,
                  const __grid_constant__ CUtensorMap tmdK, const __grid_constant__ CUtensorMap tmdV,
                  const float* __restrict__ LSE, const float* __restrict__ Delta, int T, int BH, int H, uint32_t orders,
-                 int n_tiles, int chunk, float scale, int* __restrict__ dev_status, const Window win) {
+                 int n_tiles, int chunk, float scale, int* __restrict__ dev_status, const Window win, const KvParts parts,
+                 float* __restrict__ partial) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     if (smem != smem_raw) {
@@ -574,7 +624,7 @@ attn_dkdv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     }
     KvBars* bars = reinterpret_cast<KvBars*>(smem + kOffBar);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const KvWork<kWindow> wk{BH, n_tiles, chunk, T, H, orders, kCausal, win};
+    const KvWork<kWindow> wk{BH, n_tiles, chunk, T, H, orders, kCausal, win, parts};
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < 2; ++s) {
@@ -626,7 +676,7 @@ attn_dkdv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     } else if (warp == 2) {
         kv_row_loader(bars, reinterpret_cast<float*>(smem + kOffRow), LSE, Delta, wk, lane);
     } else if (warp >= 12) {
-        kv_write_out<kStrided, kWindow>(smem, bars, tmem_base, &tmdK, &tmdV, scale, wk, warp & 3, lane);
+        kv_write_out<kStrided, kWindow>(smem, bars, tmem_base, &tmdK, &tmdV, partial, scale, wk, warp & 3, lane);
     } else if (warp >= 4) {
         kv_compute<kCausal, kWindow>(smem, bars, tmem_base, scale, wk, (warp - 4) >> 2, warp & 3, lane);
     }
@@ -652,38 +702,32 @@ cudaError_t configure_attn_dkdv() {
     return e;
 }
 
-namespace {
-// BH: heads of K and V in all, H: in a sequence.
-cudaError_t launch_dkdv(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
-                        const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided, uint32_t orders, const float* LSE,
-                        const float* Delta, const AttnShape& s, int H, const Window* win, int num_sms, int* dev_status,
-                        cudaStream_t stream) {
-    const int n_tiles = (s.T + kBlockK - 1) / kBlockK, BH = s.B * H;
-    const int chunk = heads_per_chunk(BH, n_tiles, s.T, D, num_sms);
-    const dim3 grid(static_cast<unsigned>(n_tiles) * BH);  // one CTA per item; those that do not start are taken over
-    auto go = [&](auto kernel) {
-        return launch_overlapped(kernel, grid, dim3(kThreads), kSmemBytes, stream, tmQ, tmK, tmV, tmdO, tmdK, tmdV, LSE, Delta,
-                                 s.T, BH, H, orders, n_tiles, chunk, s.scale, dev_status, win != nullptr ? *win : Window{});
-    };
-    if (win != nullptr) return strided ? go(attn_dkdv_kernel<true, true, true>) : go(attn_dkdv_kernel<true, false, true>);
-    if (s.causal) return strided ? go(attn_dkdv_kernel<true, true, false>) : go(attn_dkdv_kernel<true, false, false>);
-    return strided ? go(attn_dkdv_kernel<false, true, false>) : go(attn_dkdv_kernel<false, false, false>);
-}
-}  // namespace
-
 cudaError_t launch_attn_dkdv(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
                              const CUtensorMap& tmdO, const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided,
                              uint32_t orders, const float* LSE, const float* Delta, const AttnShape& s, int num_sms,
                              int* dev_status, cudaStream_t stream) {
-    return launch_dkdv(tmQ, tmK, tmV, tmdO, tmdK, tmdV, strided, orders, LSE, Delta, s, s.H, nullptr, num_sms, dev_status, stream);
+    const int n_tiles = (s.T + kBlockK - 1) / kBlockK, BH = s.B * s.H;
+    const int chunk = heads_per_chunk(BH, n_tiles, s.T, D, num_sms);
+    const dim3 grid(static_cast<unsigned>(n_tiles) * BH);  // one CTA per item; those that do not start are taken over
+    auto go = [&](auto kernel) {
+        return launch_overlapped(kernel, grid, dim3(kThreads), kSmemBytes, stream, tmQ, tmK, tmV, tmdO, tmdK, tmdV, LSE, Delta,
+                                 s.T, BH, s.H, orders, n_tiles, chunk, s.scale, dev_status, Window{}, KvParts{}, nullptr);
+    };
+    if (s.causal) return strided ? go(attn_dkdv_kernel<true, true, false>) : go(attn_dkdv_kernel<true, false, false>);
+    return strided ? go(attn_dkdv_kernel<false, true, false>) : go(attn_dkdv_kernel<false, false, false>);
 }
 
 cudaError_t launch_window_dkdv(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
                                const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided, uint32_t orders, const float* LSE,
-                               const float* Delta, const AttnShape& s, const Window& win, int num_sms, int* dev_status,
-                               cudaStream_t stream) {
-    return launch_dkdv(tmQ, tmK, tmV, tmdO, tmdK, tmdV, strided, orders, LSE, Delta, s, s.H / win.group, &win, num_sms, dev_status,
-                       stream);
+                               const float* Delta, const AttnShape& s, const Window& win, const KvParts& parts, float* partial,
+                               int* dev_status, cudaStream_t stream) {
+    const int H = s.H / win.group, BH = s.B * H;
+    const dim3 grid(static_cast<unsigned>(parts.items(BH)));
+    auto go = [&](auto kernel) {
+        return launch_overlapped(kernel, grid, dim3(kThreads), kSmemBytes, stream, tmQ, tmK, tmV, tmdO, tmdK, tmdV, LSE, Delta,
+                                 s.T, BH, H, orders, parts.n_tiles, BH, s.scale, dev_status, win, parts, partial);
+    };
+    return strided ? go(attn_dkdv_kernel<true, true, true>) : go(attn_dkdv_kernel<true, false, true>);
 }
 
 }  // namespace nova

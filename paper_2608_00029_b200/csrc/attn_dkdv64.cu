@@ -75,24 +75,43 @@ struct Kv64Bars {
 };
 static_assert(sizeof(Kv64Bars) <= 512, "barrier block");
 
-// Work items: 128-key tiles, heaviest (first) tiles first.  kWindow: the heads are those of K and V, and an item has the steps of
-// all query heads that share its head, one after another.
+// Work items: 128-key tiles, heaviest (first) tiles first.  kWindow: the heads are those of K and V, and the list of a tile has the
+// steps of all query heads that share its head, one after another; an item is a part of it (KvParts).
 template <bool kWindow>
 struct Kv64Work {
     int BH, T, H;
     uint32_t orders;  // coordinate orders of the Q, K, V, dO, dK, dV tensor maps, four bits each
     bool causal;
     Window win;
-    // Steps of one query head in an item of n.
+    KvParts parts;
+    // First step of item `idx` in its tile's list, and its slot of the workspace (-1: none).
+    __device__ __forceinline__ int offset(int idx) const {
+        if (!kWindow || kv_parts_of(parts, BH, idx) == 1) return 0;
+        const KvItem it = kv_item(parts, BH, idx);
+        int first, n;
+        kv_part(win.group * query_steps(win, it.kt * kBlockK, kBlockK, T, kStep), it.part, it.parts, &first, &n);
+        return first;
+    }
+    __device__ __forceinline__ int slot(int idx) const { return kWindow && kv_parts_of(parts, BH, idx) > 1 ? kv_item(parts, BH, idx).slot : -1; }
+    // Steps of one query head in the list of a tile (of n steps without the window).
     __device__ __forceinline__ int per_head(int kt, int n) const {
         return kWindow ? query_steps(win, kt * kBlockK, kBlockK, T, kStep) : n;
     }
     // Key tile, head, first step and number of steps of item `idx`.
     __device__ __forceinline__ void get(int idx, int* kt, int* bh, int* s0, int* n) const {
+        if constexpr (kWindow) {
+            const KvItem it = kv_item(parts, BH, idx);
+            *kt = it.kt;
+            *bh = it.bh;
+            *s0 = it.kt * (kBlockK / kStep);
+            int first;
+            kv_part(win.group * query_steps(win, it.kt * kBlockK, kBlockK, T, kStep), it.part, it.parts, &first, n);
+            return;
+        }
         *kt = idx / BH;
         *bh = idx - *kt * BH;
         *s0 = causal ? *kt * (kBlockK / kStep) : 0;
-        *n = kWindow ? win.group * query_steps(win, *kt * kBlockK, kBlockK, T, kStep) : (T + kStep - 1) / kStep - *s0;
+        *n = (T + kStep - 1) / kStep - *s0;
     }
 };
 
@@ -163,7 +182,9 @@ __device__ __forceinline__ void kv64_producer(const CUtensorMap* tmQ, const CUte
         tma_load_tile<kStrided>(smem + kOffV + ks * kTileBytes, tmV, &bars->kv_full[ks], (wk.orders >> 8) & 15, 0,
                                 kt * kBlockK, head, batch, bh);
         const int per = wk.per_head(kt, n);
-        int q_head = kWindow ? head * wk.win.group : head, q_bh = kWindow ? bh * wk.win.group : bh, sh = 0;
+        const int off = wk.offset(item), first = kWindow ? off / per : 0;  // the item's first query head of those that share
+        int q_head = kWindow ? head * wk.win.group + first : head, q_bh = kWindow ? bh * wk.win.group + first : bh;
+        int sh = off - first * per;
         for (int s = 0; s < n; ++s) {
             ok = mbar_wait(&bars->q_empty[st], ph ^ 1, abort_flag);
             if (!ok) break;
@@ -355,8 +376,9 @@ __device__ __forceinline__ void kv64_compute(Kv64Bars* bars, uint32_t tmem_base,
             ok = (n == 0);
             break;
         }
-        const int kt = kWindow ? item / wk.BH : 0, per = wk.per_head(kt, n);
-        int sh = (g ^ grp) & 1;  // the step in its query head
+        const int kt = kWindow ? kv_item(wk.parts, wk.BH, item).kt : 0, per = wk.per_head(kt, n);
+        int sh = 0;  // the step in its query head
+        if constexpr (kWindow) sh = (wk.offset(item) + ((g ^ grp) & 1)) % per;
         for (int s = (g ^ grp) & 1; s < n; s += 2, sh += 2, ph ^= 1) {
             if constexpr (kWindow)
                 while (sh >= per) sh -= per;
@@ -442,8 +464,8 @@ __device__ __forceinline__ void kv64_compute(Kv64Bars* bars, uint32_t tmem_base,
 // later ones only after dV and dK have been read out.
 template <bool kStrided, bool kTerms, bool kWindow>
 __device__ __forceinline__ void kv64_edges(uint8_t* smem, Kv64Bars* bars, uint32_t tmem_base, const CUtensorMap* tmdK,
-                                           const CUtensorMap* tmdV, const float* __restrict__ LSE,
-                                           const float* __restrict__ Delta, float scale, const Kv64Work<kWindow>& wk, int ow,
+                                           const CUtensorMap* tmdV, float* __restrict__ partial,
+                                           const float* __restrict__ LSE, const float* __restrict__ Delta, float scale, const Kv64Work<kWindow>& wk, int ow,
                                            int lane) {
     volatile int* abort_flag = &bars->abort_flag;
     const uint32_t lane_base = 32u * ow;
@@ -512,10 +534,32 @@ __device__ __forceinline__ void kv64_edges(uint8_t* smem, Kv64Bars* bars, uint32
         return true;
     };
     // dV and dK of the w-th item
-    auto write_out = [&](int w, int kt, int bh) -> bool {
+    int whole = 0;  // kWindow: items whose dV and dK have gone out as bf16
+    auto write_out = [&](int w, int kt, int bh, int slot) -> bool {
         if (!mbar_wait(&bars->dkv_full, w & 1, abort_flag)) return false;
         tc_fence_after();
         __syncwarp();
+        if constexpr (kWindow) {
+            if (slot >= 0) {  // a part of a tile: the sums as they are, rows past the end of the sequence among them
+                float* const to = partial + (static_cast<size_t>(slot) * 2 * kBlockK + r) * D;
+#pragma unroll
+                for (int cb = 0; cb < 2 * D; cb += 32) {
+                    uint32_t a[32];
+                    tmem_ld_x32(tmem_addr(tmem_base, lane_base, cb < D ? kColdV + cb : kColdK + cb - D), a);
+                    tmem_wait_ld();
+                    float4* const p = reinterpret_cast<float4*>(to + (cb < D ? cb : kBlockK * D + cb - D));
+#pragma unroll
+                    for (int x = 0; x < 8; ++x)
+                        p[x] = make_float4(__uint_as_float(a[4 * x]), __uint_as_float(a[4 * x + 1]), __uint_as_float(a[4 * x + 2]),
+                                           __uint_as_float(a[4 * x + 3]));
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars->dkv_free);
+                __syncwarp();
+                return true;
+            }
+        }
         uint32_t pk[2][32];
 #pragma unroll
         for (int which = 0; which < 2; ++which) {
@@ -538,7 +582,7 @@ __device__ __forceinline__ void kv64_edges(uint8_t* smem, Kv64Bars* bars, uint32
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&bars->dkv_free);
-        if (!mbar_wait(&bars->stage_free, w & 1, abort_flag)) return false;
+        if (!mbar_wait(&bars->stage_free, (kWindow ? whole : w) & 1, abort_flag)) return false;
 #pragma unroll
         for (int which = 0; which < 2; ++which)
 #pragma unroll
@@ -550,7 +594,7 @@ __device__ __forceinline__ void kv64_edges(uint8_t* smem, Kv64Bars* bars, uint32
         if (lane == 0) mbar_arrive(&bars->staged);
         bool leader_ok = true;
         if (leader) {
-            leader_ok = mbar_wait(&bars->staged, w & 1, abort_flag);
+            leader_ok = mbar_wait(&bars->staged, (kWindow ? whole : w) & 1, abort_flag);
             if (leader_ok) {
                 const int hh = kStrided ? bh % wk.H : 0, bb = kStrided ? bh / wk.H : 0;
                 tma_store_tile<kStrided>(tmdV, smem + kOffOut, (wk.orders >> 20) & 15, 0, kt * kBlockK, hh, bb, bh);
@@ -558,15 +602,16 @@ __device__ __forceinline__ void kv64_edges(uint8_t* smem, Kv64Bars* bars, uint32
                 bulk_commit_group();
             }
         }
+        if constexpr (kWindow) ++whole;
         return __all_sync(0xffffffffu, leader_ok);
     };
 
-    int g0 = 0, kt_out = 0, bh_out = 0;
+    int g0 = 0, kt_out = 0, bh_out = 0, slot_out = -1;
     for (int w = 0; ok; ++w) {
         int item = 0;
         const int taken = bars->ring.take_steps(w, lane, abort_flag, &item);
         if (taken <= 0) {
-            if (taken == 0 && w > 0) (void)write_out(w - 1, kt_out, bh_out);
+            if (taken == 0 && w > 0) (void)write_out(w - 1, kt_out, bh_out, slot_out);
             break;
         }
         int kt, bh, s0, n;
@@ -575,10 +620,11 @@ __device__ __forceinline__ void kv64_edges(uint8_t* smem, Kv64Bars* bars, uint32
         if (ok) ok = operand(w, 0);
         if (ok) ok = operand(w, 1);
         if (ok && !kTerms) ok = rows(bh, s0, g0, 2, min(n, kQStages));
-        if (ok && w > 0) ok = write_out(w - 1, kt_out, bh_out);
+        if (ok && w > 0) ok = write_out(w - 1, kt_out, bh_out, slot_out);
         if (ok && !kTerms) ok = rows(bh, s0, g0, kQStages, n);
         kt_out = kt;
         bh_out = bh;
+        slot_out = wk.slot(item);
         g0 += n;
     }
     if (leader) bulk_wait_group<0>();  // dV and dK must be complete before the kernel ends
@@ -590,13 +636,14 @@ attn_dkdv64_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                    const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmdO,
                    const __grid_constant__ CUtensorMap tmdK, const __grid_constant__ CUtensorMap tmdV,
                    const float* __restrict__ LSE, const float* __restrict__ Delta, const uint8_t* __restrict__ terms, int T, int BH,
-                   int H, uint32_t orders, float scale, int* __restrict__ dev_status, const Window win) {
+                   int H, uint32_t orders, float scale, int* __restrict__ dev_status, const Window win, const KvParts parts,
+                   float* __restrict__ partial) {
     static_assert(!kWindow || (kCausal && kTerms), "with the window the row terms are prepared");
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     Kv64Bars* bars = reinterpret_cast<Kv64Bars*>(smem + kOffBar);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Kv64Work<kWindow> wk{BH, T, H, orders, kCausal, win};
+    const Kv64Work<kWindow> wk{BH, T, H, orders, kCausal, win, parts};
 
     // The kernel before this one in the stream is the dQ kernel, of which nothing is needed: it need not have completed (ptx.cuh).
     // The threads that will read global memory, the producer and the edge warps, see to it while the others set up.
@@ -664,7 +711,7 @@ attn_dkdv64_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     } else if (warp == 3) {
         kv64_mma_acc(smem, bars, tmem_base);
     } else if (warp >= 12) {
-        kv64_edges<kStrided, kTerms, kWindow>(smem, bars, tmem_base, &tmdK, &tmdV, LSE, Delta, scale, wk, warp & 3, lane);
+        kv64_edges<kStrided, kTerms, kWindow>(smem, bars, tmem_base, &tmdK, &tmdV, partial, LSE, Delta, scale, wk, warp & 3, lane);
     } else {
         kv64_compute<kCausal, kWindow>(bars, tmem_base, scale, wk, (warp - 4) >> 2, warp & 3, lane);
     }
@@ -701,41 +748,35 @@ cudaError_t launch_row_terms64(const float* LSE, const float* Delta, void* terms
                              static_cast<uint8_t*>(terms), s.T, n_steps, rows, 1.0f / fmaxf(s.scale, kLeastScale));
 }
 
-namespace {
-// H: heads of K and V in a sequence.
-cudaError_t launch_dkdv64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
-                          const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided, uint32_t orders, const float* LSE,
-                          const float* Delta, const void* terms, const AttnShape& s, int H, const Window* win, int* dev_status,
-                          cudaStream_t stream) {
-    if ((strided || win != nullptr) && terms == nullptr) return cudaErrorNotSupported;  // (only the deterministic entry point has no workspace)
-    const int n_tiles = (s.T + kBlockK - 1) / kBlockK, BH = s.B * H;
+cudaError_t launch_attn_dkdv64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
+                               const CUtensorMap& tmdO, const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided,
+                               uint32_t orders, const float* LSE, const float* Delta, const void* terms, const AttnShape& s,
+                               int* dev_status, cudaStream_t stream) {
+    if (strided && terms == nullptr) return cudaErrorNotSupported;  // (only the deterministic entry point has no workspace)
+    const int n_tiles = (s.T + kBlockK - 1) / kBlockK, BH = s.B * s.H;
     const dim3 grid(static_cast<unsigned>(n_tiles) * BH);  // one CTA per item; those that do not start are taken over
     auto go = [&](auto kernel) {
         return launch_overlapped(kernel, grid, dim3(kThreads), kSmemBytes, stream, tmQ, tmK, tmV, tmdO, tmdK, tmdV, LSE, Delta,
-                                 static_cast<const uint8_t*>(terms), s.T, BH, H, orders, s.scale, dev_status,
-                                 win != nullptr ? *win : Window{});
+                                 static_cast<const uint8_t*>(terms), s.T, BH, s.H, orders, s.scale, dev_status, Window{}, KvParts{},
+                                 nullptr);
     };
-    if (win != nullptr) return strided ? go(attn_dkdv64_kernel<true, true, true, true>) : go(attn_dkdv64_kernel<true, false, true, true>);
     if (terms == nullptr)
         return s.causal ? go(attn_dkdv64_kernel<true, false, false, false>) : go(attn_dkdv64_kernel<false, false, false, false>);
     if (s.causal) return strided ? go(attn_dkdv64_kernel<true, true, true, false>) : go(attn_dkdv64_kernel<true, false, true, false>);
     return strided ? go(attn_dkdv64_kernel<false, true, true, false>) : go(attn_dkdv64_kernel<false, false, true, false>);
 }
-}  // namespace
-
-cudaError_t launch_attn_dkdv64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,
-                               const CUtensorMap& tmdO, const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided,
-                               uint32_t orders, const float* LSE, const float* Delta, const void* terms, const AttnShape& s,
-                               int* dev_status, cudaStream_t stream) {
-    return launch_dkdv64(tmQ, tmK, tmV, tmdO, tmdK, tmdV, strided, orders, LSE, Delta, terms, s, s.H, nullptr, dev_status, stream);
-}
 
 cudaError_t launch_window_dkdv64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
                                  const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided, uint32_t orders, const float* LSE,
-                                 const float* Delta, const void* terms, const AttnShape& s, const Window& win, int* dev_status,
-                                 cudaStream_t stream) {
-    return launch_dkdv64(tmQ, tmK, tmV, tmdO, tmdK, tmdV, strided, orders, LSE, Delta, terms, s, s.H / win.group, &win, dev_status,
-                         stream);
+                                 const float* Delta, const void* terms, const AttnShape& s, const Window& win, const KvParts& parts,
+                                 float* partial, int* dev_status, cudaStream_t stream) {
+    const int H = s.H / win.group, BH = s.B * H;
+    const dim3 grid(static_cast<unsigned>(parts.items(BH)));
+    auto go = [&](auto kernel) {
+        return launch_overlapped(kernel, grid, dim3(kThreads), kSmemBytes, stream, tmQ, tmK, tmV, tmdO, tmdK, tmdV, LSE, Delta,
+                                 static_cast<const uint8_t*>(terms), s.T, BH, H, orders, s.scale, dev_status, win, parts, partial);
+    };
+    return strided ? go(attn_dkdv64_kernel<true, true, true, true>) : go(attn_dkdv64_kernel<true, false, true, true>);
 }
 
 }  // namespace nova

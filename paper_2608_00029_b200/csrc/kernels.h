@@ -50,6 +50,53 @@ __host__ __device__ __forceinline__ int query_steps(const Window& w, int k0, int
     return (end - 1) / unit + 1 - k0 / unit;
 }
 
+// Items of the dK/dV kernels with the window.  A key tile's list of steps (all query heads that share its head, one after another) is
+// dealt out to `parts` items of equal length, or with sinks in the tile `sink_parts`: those lists end with the sequence.  Where there
+// is more than one part each writes its sums, in 32 bits, to a slot of the workspace ([2][128][D]: dV, dK), and
+// launch_window_sum adds them up.  One order of sums for all of a shape's calls.
+struct KvParts {
+    int n_tiles, sink_tiles, sink_parts, parts;  // tiles of a head; the first ones, which hold sinks
+    __host__ __device__ __forceinline__ long long items(long long BH) const {
+        return BH * (static_cast<long long>(sink_tiles) * sink_parts + static_cast<long long>(n_tiles - sink_tiles) * parts);
+    }
+    __host__ __device__ __forceinline__ long long slots(long long BH) const {
+        return BH * ((sink_parts > 1 ? static_cast<long long>(sink_tiles) * sink_parts : 0) +
+                     (parts > 1 ? static_cast<long long>(n_tiles - sink_tiles) * parts : 0));
+    }
+};
+// How many parts the tile of item `idx` has.
+__host__ __device__ __forceinline__ int kv_parts_of(const KvParts& p, int BH, int idx) {
+    return idx < p.sink_tiles * p.sink_parts * BH ? p.sink_parts : p.parts;
+}
+struct KvItem {
+    int kt, bh, part, parts, slot;  // slot: -1 without one
+};
+// Item `idx` of a problem with BH heads of K and V: tile by tile, the first (longest) ones first.
+__host__ __device__ __forceinline__ KvItem kv_item(const KvParts& p, int BH, int idx) {
+    const int first = p.sink_tiles * p.sink_parts * BH;
+    const bool sink = idx < first;
+    KvItem it;
+    it.parts = sink ? p.sink_parts : p.parts;
+    const int in = sink ? idx : idx - first, per_tile = it.parts * BH, tile = in / per_tile, rem = in - tile * per_tile;
+    it.kt = (sink ? 0 : p.sink_tiles) + tile;
+    it.part = it.parts == 1 ? 0 : rem / BH;
+    it.bh = rem - it.part * BH;
+    it.slot = it.parts == 1 ? -1 : sink ? idx : in + (p.sink_parts > 1 ? first : 0);
+    return it;
+}
+// Steps [first, first + n) of a list of `all` that a part has.
+__host__ __device__ __forceinline__ void kv_part(int all, int part, int parts, int* first, int* n) {
+    *first = 0;
+    *n = all;
+    if (parts == 1) return;
+    *first = static_cast<int>(static_cast<long long>(all) * part / parts);
+    *n = static_cast<int>(static_cast<long long>(all) * (part + 1) / parts) - *first;
+}
+// BH: heads of K and V in all.  Of the shape alone.
+KvParts kv_parts(int BH, int T, const Window& win);
+cudaError_t launch_window_sum(const float* partial, const KvParts& parts, __nv_bfloat16* dK, __nv_bfloat16* dV, const TensorStrides& sdk,
+                              const TensorStrides& sdv, int B, int H_kv, int T, int D, float scale, cudaStream_t stream);
+
 #ifdef __CUDACC__
 // Bits 0 .. n - 1 of 64.
 __device__ __forceinline__ uint64_t bits_below(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }
@@ -160,8 +207,8 @@ cudaError_t launch_attn_dkdv(const CUtensorMap& tmQ, const CUtensorMap& tmK, con
 // With the window: dK and dV have the heads of K and V, an item all query heads that share its key/value head.
 cudaError_t launch_window_dkdv(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
                                const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided, uint32_t orders, const float* LSE,
-                               const float* Delta, const AttnShape& s, const Window& win, int num_sms, int* dev_status,
-                               cudaStream_t stream);
+                               const float* Delta, const AttnShape& s, const Window& win, const KvParts& parts, float* partial,
+                               int* dev_status, cudaStream_t stream);
 cudaError_t configure_attn_dkdv();
 // The same at D = 64 (attn_dkdv64.cu).  `terms`: the row terms of every query as launch_row_terms64 leaves them (32 bytes for
 // each of B * H * ceil(T / 64) * 64 rows, 16-byte aligned), or null: the kernel makes them itself (plain layout only).  Goes out
@@ -173,8 +220,8 @@ cudaError_t launch_attn_dkdv64(const CUtensorMap& tmQ, const CUtensorMap& tmK, c
                                int* dev_status, cudaStream_t stream);
 cudaError_t launch_window_dkdv64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
                                  const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided, uint32_t orders, const float* LSE,
-                                 const float* Delta, const void* terms, const AttnShape& s, const Window& win, int* dev_status,
-                                 cudaStream_t stream);
+                                 const float* Delta, const void* terms, const AttnShape& s, const Window& win, const KvParts& parts,
+                                 float* partial, int* dev_status, cudaStream_t stream);
 cudaError_t configure_attn_dkdv64();
 
 // Heads that the items of the kernels at D=128 are taken in together: enough items for two rounds of the SMs, and no more

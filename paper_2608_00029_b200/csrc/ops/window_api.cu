@@ -22,10 +22,16 @@ size_t decode_bytes(const DecodePlan& p, int B, int H, int D) {
     return p.splits == 1 ? 0 : static_cast<size_t>(B) * H * p.splits * (D + 2) * sizeof(float);
 }
 
-// The row terms of the dK/dV kernel at D = 64: 32 bytes a row, the rows of a head rounded up to kKeyStep.
-size_t bwd_bytes(int B, int H, int T, int D) {
-    const size_t rows = static_cast<size_t>(B) * H * ((T + kKeyStep - 1) / kKeyStep) * kKeyStep;
-    return std::max<size_t>(256, D == 64 ? rows * 32 : 0);
+Window window_of(int H, int H_kv, int T, int window, int sinks) { return Window{std::min(window, T), std::min(sinks, T), H / H_kv}; }
+
+// The row terms of the dK/dV kernel at D = 64 (32 bytes a row, the rows of a head rounded up to kKeyStep), then the slots of the key
+// tiles that are summed in parts.
+size_t terms_bytes(int B, int H, int T, int D) {
+    return D == 64 ? static_cast<size_t>(B) * H * ((T + kKeyStep - 1) / kKeyStep) * kKeyStep * 32 : 0;
+}
+size_t bwd_bytes(int B, int H, int H_kv, int T, int D, const KvParts& parts) {
+    const size_t slots = static_cast<size_t>(parts.slots(static_cast<long long>(B) * H_kv)) * 2 * kBlockK * D * sizeof(float);
+    return std::max<size_t>(256, terms_bytes(B, H, T, D) + slots);
 }
 
 }  // namespace
@@ -48,7 +54,7 @@ int nova_window_fwd(const void* Q, const void* K, const void* V, void* O, void* 
     DeviceState* st = nullptr;
     if (int rc = device_state(&st)) return rc;
     const AttnShape s{B, H, T, D, 1, scale}, s_kv{B, H_kv, T, D, 1, scale};
-    const Window win{std::min(window, T), std::min(sinks, T), H / H_kv};
+    const Window win = window_of(H, H_kv, T, window, sinks);
     CUtensorMap tmQ, tmK, tmV;
     uint32_t oq, ok, ov;
     const bool strided = !(merges(s, sq) && merges(s_kv, sk) && merges(s_kv, sv));
@@ -80,7 +86,7 @@ int nova_window_bwd_preprocess(const void* O, const void* O_rest, const void* dO
 
 size_t nova_window_bwd_workspace_bytes(int B, int H, int H_kv, int T, int D, int window, int sinks) {
     if (check_window(B, H, H_kv, T, D, window, sinks) != NOVA_ATTN_OK) return 0;
-    return bwd_bytes(B, H, T, D);
+    return bwd_bytes(B, H, H_kv, T, D, kv_parts(B * H_kv, T, window_of(H, H_kv, T, window, sinks)));
 }
 
 int nova_window_bwd(const void* Q, const void* K, const void* V, const void* dO, const float* LSE, const float* Delta, void* dQ, void* dK,
@@ -98,12 +104,14 @@ int nova_window_bwd(const void* Q, const void* K, const void* V, const void* dO,
     if (int rc = check_strides(dq_strides, D, &sdq)) return rc;
     if (int rc = check_strides(dk_strides, D, &sdk)) return rc;
     if (int rc = check_strides(dv_strides, D, &sdv)) return rc;
-    if (!workspace || workspace_bytes < bwd_bytes(B, H, T, D)) return NOVA_ATTN_ERR_WORKSPACE;
+    const Window win = window_of(H, H_kv, T, window, sinks);
+    const KvParts parts = kv_parts(B * H_kv, T, win);
+    if (!workspace || workspace_bytes < bwd_bytes(B, H, H_kv, T, D, parts)) return NOVA_ATTN_ERR_WORKSPACE;
+    if (parts.items(static_cast<long long>(B) * H_kv) > 0x7fffffffll) return NOVA_ATTN_ERR_SHAPE;
     if (!aligned16(workspace)) return NOVA_ATTN_ERR_ALIGNMENT;
     DeviceState* st = nullptr;
     if (int rc = device_state(&st)) return rc;
     const AttnShape s{B, H, T, D, 1, scale}, s_kv{B, H_kv, T, D, 1, scale};
-    const Window win{std::min(window, T), std::min(sinks, T), H / H_kv};
     const bool strided = !(merges(s, sq) && merges(s_kv, sk) && merges(s_kv, sv) && merges(s, sdo) && merges(s, sdq) &&
                            merges(s_kv, sdk) && merges(s_kv, sdv));
     // Each kernel takes what it streams in boxes of kKeyStep rows and what it holds in boxes of 128.
@@ -123,20 +131,23 @@ int nova_window_bwd(const void* Q, const void* K, const void* V, const void* dO,
     const uint32_t orders = oq | (ok << 4) | (ov << 8) | (odo << 12);
     const uint32_t orders_dq = orders | (odq << 16), orders_kv = orders | (odk << 16) | (odv << 20);
     const cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    float* const partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + terms_bytes(B, H, T, D));
     cudaError_t e;
     if (D == 64) {
         e = launch_row_terms64(LSE, Delta, workspace, s, cs);
         if (e == cudaSuccess)
             e = launch_window_dq64(tmQ, tmKs, tmVs, tmdO, tmdQ, strided, orders_dq, LSE, Delta, s, win, st->dev_status, cs);
         if (e == cudaSuccess)
-            e = launch_window_dkdv64(tmQs, tmK, tmV, tmdOs, tmdK, tmdV, strided, orders_kv, LSE, Delta, workspace, s, win,
-                                     st->dev_status, cs);
+            e = launch_window_dkdv64(tmQs, tmK, tmV, tmdOs, tmdK, tmdV, strided, orders_kv, LSE, Delta, workspace, s, win, parts,
+                                     partial, st->dev_status, cs);
     } else {
         e = launch_window_dq(tmQ, tmKs, tmVs, tmdO, tmdQ, strided, orders_dq, LSE, Delta, s, win, st->num_sms, st->dev_status, cs);
         if (e == cudaSuccess)
-            e = launch_window_dkdv(tmQs, tmK, tmV, tmdOs, tmdK, tmdV, strided, orders_kv, LSE, Delta, s, win, st->num_sms,
+            e = launch_window_dkdv(tmQs, tmK, tmV, tmdOs, tmdK, tmdV, strided, orders_kv, LSE, Delta, s, win, parts, partial,
                                    st->dev_status, cs);
     }
+    if (e == cudaSuccess && parts.slots(1) > 0)
+        e = launch_window_sum(partial, parts, static_cast<__nv_bfloat16*>(dK), static_cast<__nv_bfloat16*>(dV), sdk, sdv, B, H_kv, T, D, scale, cs);
     return e == cudaSuccess ? NOVA_ATTN_OK : record_cuda_error(e);
 }
 

@@ -1,0 +1,92 @@
+// How the dK/dV kernels' work with a window is cut into items (KvParts), and the sum of what the parts of a key tile found.
+#include <algorithm>
+
+#include "../api.h"
+#include "../ptx.cuh"
+
+namespace nova {
+namespace {
+
+constexpr int kThreads = 256;
+
+// Eight columns of one row of dV or dK per thread: the parts' sums in order, 32 bits, rounded once.
+template <int D>
+__global__ void __launch_bounds__(kThreads) window_sum_kernel(const float* __restrict__ partial, const KvParts parts, uint16_t* __restrict__ dK,
+                                                              uint16_t* __restrict__ dV, const TensorStrides sdk, const TensorStrides sdv,
+                                                              int BH, int H, int T, float scale) {
+    constexpr int kPerRow = D / 8, kRows = kThreads / kPerRow, kBlocks = 2 * kBlockK / kRows;  // blocks of a tile: dV, dK
+    griddep_launch_dependents();
+    const int tile_bh = blockIdx.x / kBlocks, in = blockIdx.x - tile_bh * kBlocks;
+    const int first = parts.sink_parts > 1 ? 0 : parts.sink_tiles;  // the first tile that is in parts
+    const int kt = first + tile_bh / BH, bh = tile_bh - (kt - first) * BH;
+    const int n = kt < parts.sink_tiles ? parts.sink_parts : parts.parts;
+    const int vr = in * kRows + threadIdx.x / kPerRow, which = vr / kBlockK, r = vr - which * kBlockK, c = threadIdx.x % kPerRow * 8;
+    // the slots of a tile lie BH apart
+    const long long before = kt < parts.sink_tiles ? static_cast<long long>(kt) * n * BH
+                                                   : (parts.sink_parts > 1 ? static_cast<long long>(parts.sink_tiles) * parts.sink_parts * BH : 0) +
+                                                         static_cast<long long>(kt - parts.sink_tiles) * n * BH;
+    const float* p = partial + ((before + bh) * 2 * kBlockK + vr) * D + c;
+    const size_t step = static_cast<size_t>(BH) * 2 * kBlockK * D;
+    const int row = kt * kBlockK + r;
+    griddep_wait();
+    if (row >= T) return;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+#pragma unroll 4
+    for (int i = 0; i < n; ++i, p += step) {
+        const float4 x = __ldcs(reinterpret_cast<const float4*>(p)), y = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+        a.x += x.x, a.y += x.y, a.z += x.z, a.w += x.w;
+        b.x += y.x, b.y += y.y, b.z += y.z, b.w += y.w;
+    }
+    const float f = which ? scale : 1.f;
+    const TensorStrides& s = which ? sdk : sdv;
+    const int batch = bh / H, head = bh - batch * H;
+    *reinterpret_cast<uint4*>((which ? dK : dV) + batch * s.b + head * s.h + row * s.t + c) =
+        make_uint4(pack_bf16x2(a.x * f, a.y * f), pack_bf16x2(a.z * f, a.w * f), pack_bf16x2(b.x * f, b.y * f), pack_bf16x2(b.z * f, b.w * f));
+}
+
+}  // namespace
+
+KvParts kv_parts(int BH, int T, const Window& win) {
+    constexpr int kSms = 148;
+    constexpr int kLeast = 12;  // steps of a part: below that the ends of an item cost more than its steps
+    KvParts p;
+    p.n_tiles = (T + kBlockK - 1) / kBlockK;
+    p.sink_tiles = std::min(p.n_tiles, (win.sinks + kBlockK - 1) / kBlockK);
+    p.sink_parts = p.parts = 1;
+    auto list = [&](int kt) { return static_cast<long long>(win.group) * query_steps(win, kt * kBlockK, kBlockK, T, kKeyStep); };
+    // Steps of all lists, per SM: those with sinks end with the sequence, the others are of one length until they do, too.
+    const long long n_q = (T + kKeyStep - 1) / kKeyStep, per_tile = kBlockK / kKeyStep;
+    const long long whole = (static_cast<long long>(win.window) + kBlockK - 2) / kKeyStep + 1;
+    auto to_end = [&](long long first, long long last) {  // tiles first .. last - 1
+        return first < last ? (last - first) * n_q - per_tile * (last * (last - 1) - first * (first - 1)) / 2 : 0ll;
+    };
+    const long long cut_from = std::min<long long>(p.n_tiles, std::max<long long>(p.sink_tiles, n_q >= whole ? (n_q - whole) / per_tile + 1 : 0));
+    const long long all = to_end(0, p.sink_tiles) + (cut_from - p.sink_tiles) * whole + to_end(cut_from, p.n_tiles);
+    const long long per_sm = all * win.group * BH / kSms;
+    auto cut = [&](int first, int last, long long most) -> int {  // parts of tiles whose longest list is the first, shortest the last
+        const long long n = (list(first) + most - 1) / most;
+        return static_cast<int>(std::max(1ll, std::min(n, list(last))));
+    };
+    // A tile with sinks that is longer than an SM's share of all steps: into thirds of that (B=2, H=12 on 4, T=8192, D=128, window
+    // 1024, 4 sinks: a list of 384 steps, a share of 209: 404 us in one item, 256 so).  Shorter ones go first and hold nobody up
+    // (B=8, H=12, T=1024, D=64, window 256, 4 sinks, 16 steps of 30: 29.7 us, 39 in two parts).
+    if (p.sink_tiles > 0 && list(0) > per_sm) p.sink_parts = cut(0, p.sink_tiles - 1, std::max<long long>(kLeast, per_sm / 3));
+    // The others only where there are fewer of them than SMs.
+    const long long rest = static_cast<long long>(p.n_tiles - p.sink_tiles) * BH;
+    if (rest > 0 && rest < kSms) p.parts = cut(p.sink_tiles, p.n_tiles - 1, std::max<long long>(kLeast, list(p.sink_tiles) * rest / kSms));
+    return p;
+}
+
+cudaError_t launch_window_sum(const float* partial, const KvParts& parts, __nv_bfloat16* dK, __nv_bfloat16* dV, const TensorStrides& sdk,
+                              const TensorStrides& sdv, int B, int H_kv, int T, int D, float scale, cudaStream_t stream) {
+    const int BH = B * H_kv;
+    const long long tiles = static_cast<long long>(parts.sink_parts > 1 ? parts.sink_tiles : 0) + (parts.parts > 1 ? parts.n_tiles - parts.sink_tiles : 0);
+    const dim3 grid(static_cast<unsigned>(tiles * BH * (2 * kBlockK * (D / 8) / kThreads)));
+    auto go = [&](auto kernel) {
+        return launch_overlapped(kernel, grid, dim3(kThreads), 0, stream, partial, parts, reinterpret_cast<uint16_t*>(dK),
+                                 reinterpret_cast<uint16_t*>(dV), sdk, sdv, BH, H_kv, T, scale);
+    };
+    return D == 64 ? go(window_sum_kernel<64>) : go(window_sum_kernel<128>);
+}
+
+}  // namespace nova

@@ -121,6 +121,10 @@ SHAPES = [
     (20, 6, 3, 260, 128, 40, 1),
     (3, 12, 4, 640, 64, 64, 4),
     (1, 64, 2, 300, 64, 90, 7),
+    (1, 8, 1, 3000, 64, 100, 4),      # the sinks' tile, and the others, in parts
+    (1, 6, 2, 2600, 128, 300, 200),   # two tiles with sinks
+    (2, 12, 1, 1100, 128, 1100, 0),   # long lists on few heads
+    (1, 16, 1, 200, 64, 200, 0),
 ]
 
 

@@ -175,6 +175,18 @@ void span(int window, int sinks, int q0, int rows, int T, int unit, int* out) {
 int steps(int window, int sinks, int k0, int keys, int T, int unit) {
     return nova::query_steps(nova::Window{window, sinks, 1}, k0, keys, T, unit);
 }
+// kt, bh, part, parts, slot, first step, steps
+void item(int n_tiles, int sink_tiles, int sink_parts, int parts, int BH, int idx, int all, int* out) {
+    const nova::KvItem it = nova::kv_item(nova::KvParts{n_tiles, sink_tiles, sink_parts, parts}, BH, idx);
+    out[0] = it.kt, out[1] = it.bh, out[2] = it.part, out[3] = it.parts, out[4] = it.slot;
+    nova::kv_part(all, it.part, it.parts, out + 5, out + 6);
+}
+long long slots(int n_tiles, int sink_tiles, int sink_parts, int parts, int BH) {
+    return nova::KvParts{n_tiles, sink_tiles, sink_parts, parts}.slots(BH);
+}
+long long items(int n_tiles, int sink_tiles, int sink_parts, int parts, int BH) {
+    return nova::KvParts{n_tiles, sink_tiles, sink_parts, parts}.items(BH);
+}
 }
 """
 
@@ -205,6 +217,31 @@ def test_tiles_visited_are_those_with_something_kept(spans):
                     n = spans.steps(window_, sinks_, k0, rows, T, unit)
                     kept = [q // unit for q in range(0, T, unit) if m[q:q + unit, k0:k0 + rows].any()]
                     assert k0 // unit == kept[0] and k0 // unit + n - 1 == kept[-1], (T, window, sinks, k0)
+
+
+def test_every_part_of_every_tile_is_dealt_out_once(spans):
+    out = (ctypes.c_int * 7)()
+    spans.slots.restype = spans.items.restype = ctypes.c_longlong
+    for n_tiles, sink_tiles, sink_parts, parts, BH in ((1, 0, 1, 1, 1), (7, 1, 5, 1, 6), (9, 2, 3, 4, 2), (5, 0, 1, 8, 3), (6, 6, 4, 1, 2), (8, 3, 1, 2, 5)):
+        seen, slots = {}, []
+        for idx in range(spans.items(n_tiles, sink_tiles, sink_parts, parts, BH)):
+            spans.item(n_tiles, sink_tiles, sink_parts, parts, BH, idx, 37, out)
+            kt, bh, part, of, slot, first, n = out
+            assert 0 <= kt < n_tiles and 0 <= bh < BH and of == (sink_parts if kt < sink_tiles else parts)
+            assert n >= 37 // of and (slot >= 0) == (of > 1)
+            seen.setdefault((kt, bh), []).append((first, n))
+            slots += [slot] if slot >= 0 else []
+            if slot >= 0:  # where window_sum_kernel looks for it: a tile's parts BH apart
+                before = kt * of * BH if kt < sink_tiles else (sink_tiles * sink_parts * BH if sink_parts > 1 else 0) + (kt - sink_tiles) * of * BH
+                assert slot == before + bh + part * BH
+        assert len(seen) == n_tiles * BH
+        for parts_of in seen.values():
+            at = 0
+            for first, n in sorted(parts_of):
+                assert first == at
+                at += n
+            assert at == 37
+        assert sorted(slots) == list(range(spans.slots(n_tiles, sink_tiles, sink_parts, parts, BH)))
 
 
 def test_kernels_of_the_subfolder_wait_for_their_predecessor():
