@@ -281,26 +281,31 @@ __device__ __forceinline__ void softmax(Bars* bars, uint32_t tmem_base, uint16_t
     const int T = wk.T;
     bool ok = true;
     int g = 0;  // steps of all items
-    for (int w = 0;; ++w) {
-        const int item = bars->ring.take(w, lane, abort_flag, kWaitLimitCycles);
-        if (item < 0) return;
+    int item = bars->ring.take(0, lane, abort_flag, kWaitLimitCycles);
+    for (int w = 0; item >= 0; ++w) {
         int qt, bh;
         KeySpan span;
         wk.get(item, &qt, &bh, &span);
         const int row0 = qt * kBlockQ + lane_base, row = row0 + lane;  // the warp's first row, the thread's
         const int last = min(row0 + 31, T - 1), kept_row = min(row, T - 1);
         float m_ref = -INFINITY, l = 0.f;  // -inf while there has been no key that the row keeps
-        for (int j = 0; j < span.n; ++j, ++g) {
-            const int buf = g & 1, key0 = span.at(j) * kStep;
-            const uint32_t t_s = tmem_addr(tmem_base, lane_base, C::kColS + kStep * buf);
-            // Halves of 32 keys: does any of the warp's rows keep any of it, and all of them all of it?  The same in every lane.
-            bool need[2], whole[2];
+        // Halves of 32 keys: does any of the warp's rows keep any of it, and all of them all of it?  The same in every lane.  (Found out
+        // for a step while the P of the one before is on its way.)
+        int key0;
+        bool need[2], whole[2];
+        auto look = [&](int j) {
+            key0 = span.at(j) * kStep;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int k0 = key0 + 32 * h;
                 need[h] = k0 <= last && (k0 + 31 > row0 - wk.win.window || k0 < wk.win.sinks);
                 whole[h] = k0 + 31 <= row0 && (k0 > row0 + 31 - wk.win.window || k0 + 31 < wk.win.sinks);
             }
+        };
+        look(0);
+        for (int j = 0; j < span.n; ++j, ++g) {
+            const int buf = g & 1;
+            const uint32_t t_s = tmem_addr(tmem_base, lane_base, C::kColS + kStep * buf);
             ok = mbar_wait(&bars->s_full[buf], (g >> 1) & 1, abort_flag);
             if (!ok) break;
             tc_fence_after();
@@ -363,8 +368,8 @@ __device__ __forceinline__ void softmax(Bars* bars, uint32_t tmem_base, uint16_t
                         const float p0 = ex2_approx(x0), p1 = ex2_approx(x1), p2 = ex2_approx(x2), p3 = ex2_approx(x3);
                         acc[i / 2 % 4] = f32x2_add(acc[i / 2 % 4], f32x2_pack(p0, p1));
                         acc[i / 2 % 4 + 1] = f32x2_add(acc[i / 2 % 4 + 1], f32x2_pack(p2, p3));
-                        pk[i / 2] = pack_bf16x2_int(p0, p1);
-                        pk[i / 2 + 1] = pack_bf16x2_int(p2, p3);
+                        pk[i / 2] = pack_bf16x2(p0, p1);
+                        pk[i / 2 + 1] = pack_bf16x2(p2, p3);
                     }
                 } else {
 #pragma unroll
@@ -376,20 +381,22 @@ __device__ __forceinline__ void softmax(Bars* bars, uint32_t tmem_base, uint16_t
             f32x2_unpack(f32x2_add(acc[0], acc[2]), a0, a1);
             f32x2_unpack(f32x2_add(acc[1], acc[3]), a2, a3);
             l += (a0 + a1) + (a2 + a3);
+            look(j + 1);  // (past the last step it says nothing)
             tmem_wait_st();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&bars->p_ready[buf]);
         }
         if (!ok) return;
-        // ---- end of the item.  (Not pv_done: P V of the step before the last may be outstanding still, and a wait two phases on
-        // would pass at once.)
-        ok = mbar_wait(&bars->o_done, w & 1, abort_flag);
-        if (!ok) return;
-        tc_fence_after();
+        // ---- end of the item: what needs no O first, then O
+        item = bars->ring.take(w + 1, lane, abort_flag, kWaitLimitCycles);
         const float inv_l = 1.0f / l;
         const long long b = bh / wk.H, at = b * so.b + (bh - b * wk.H) * so.h + row * so.t;
         if (row < T) LSE[static_cast<size_t>(bh) * T + row] = m_ref * scale + logf(l);
+        // (Not pv_done: P V of the step before the last may be outstanding still, and a wait two phases on would pass at once.)
+        ok = mbar_wait(&bars->o_done, w & 1, abort_flag);
+        if (!ok) return;
+        tc_fence_after();
 #pragma unroll
         for (int cb = 0; cb < D; cb += 32) {
             uint32_t a[32], v[16], r[16];
