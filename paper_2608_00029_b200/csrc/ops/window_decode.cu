@@ -5,12 +5,13 @@
 // warps every fourth 16 of them; what a CTA finds, its maximum, sum and weighted sum per query head, is joined with the
 // other runs' by a second kernel unless one run holds all.
 //
-// The two products go through the warp-level tensor instruction (m16n8k16), query heads as the rows: not for its rate, of which
-// they need a tenth, but because the dot products of G heads with one key would otherwise be 4 G shuffles.  Its operands come
-// straight from global memory, 16 bytes a load: which of the D dimensions, or of the keys, an instruction counts as which is
-// free as long as both operands agree.
-//   scores  the lane's 16 bytes of a key, dimensions 32 i + 8 (lane % 4) + 0..7, are its shares of two instructions
-//   values  the lane's 16 bytes of four keys are columns of eight instructions, keys paired by byte permutes
+// The two products go through the warp-level tensor instruction (m16n8k16), keys or dimensions as its 16 rows, query heads as its 8
+// columns: not for its rate, of which they need a tenth, but because the dot products of G heads with one key would otherwise be
+// 4 G shuffles.  Its operands come straight from global memory, 16 bytes a load: which of the D dimensions, or of the keys, an
+// instruction counts as which is free as long as both operands agree.
+//   scores  S^T = K Q^T: the lane's 16 bytes of a key, dimensions 32 i + 8 (lane % 4) + 0..7, are its shares of two instructions
+//   values  O^T = V^T P^T: the lane's 16 bytes of four keys are two rows each of four instructions, keys paired by byte permutes;
+//           P^T is the transpose of what the first product leaves in the lanes (movmatrix)
 // The weights enter the second product as two bf16 numbers each, which together keep 16 bits of them: rounded to one, they
 // would cost as much accuracy as the rounding of the output does.
 #include <cmath>
@@ -39,11 +40,19 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t& hi, uint3
     lo = pack_bf16x2(x - __uint_as_float(hi << 16), y - __uint_as_float(hi & 0xffff0000u));
 }
 
-// kWide: more than 8 query heads, rows 8 to 15 of the instructions are in use.
-template <int D, bool kWide>
-__global__ void __launch_bounds__(kThreads) window_decode_kernel(const __grid_constant__ DecodeArgs a) {
-    __shared__ float s_o[kWarps][kWide ? 16 : 8][D];
-    __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
+// 8x8 matrix of 16-bit numbers, a row in four lanes: its transpose.
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+// kCols: groups of 8 query heads.
+template <int D, int kCols>
+__global__ void __launch_bounds__(kThreads, kCols == 1 ? (D == 64 ? 5 : 3) : (D == 64 ? 3 : 2))
+window_decode_kernel(const __grid_constant__ DecodeArgs a) {
+    __shared__ float s_o[kWarps][8 * kCols][D + 4];  // (rows of a warp's eight lanes in different banks)
+    __shared__ float s_m[kWarps][8 * kCols], s_l[kWarps][8 * kCols];
     griddep_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3, oct = lane >> 2;
     const int item = blockIdx.x / a.splits, split = blockIdx.x - item * a.splits;
@@ -55,21 +64,18 @@ __global__ void __launch_bounds__(kThreads) window_decode_kernel(const __grid_co
     const int e0 = split * a.chunk, e1 = min(keys.n, e0 + a.chunk);
     if (e0 >= e1 && !(split == 0 && a.splits == 1)) return;  // (a run that is not there is not looked for either)
 
-    // Q as the first operand: rows oct and oct + 8
-    uint32_t qa[D / 32][4], qb[D / 32][4];
+    // Q^T as the second operand: column oct of each group of heads
+    uint4 qr[kCols][D / 32];
     const uint16_t* const q = a.q + b * a.sq.b + h0 * a.sq.h + 8 * quad;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-        uint4 x = make_uint4(0, 0, 0, 0), y = x;
-        if (oct < rows) x = *reinterpret_cast<const uint4*>(q + oct * a.sq.h + 32 * i);
-        if (kWide && oct + 8 < rows) y = *reinterpret_cast<const uint4*>(q + (oct + 8) * a.sq.h + 32 * i);
-        qa[i][0] = x.x, qa[i][1] = x.y, qa[i][2] = x.z, qa[i][3] = x.w;
-        qb[i][0] = y.x, qb[i][1] = y.y, qb[i][2] = y.z, qb[i][3] = y.w;
-    }
+    for (int n = 0; n < kCols; ++n)
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+            qr[n][i] = 8 * n + oct < rows ? *reinterpret_cast<const uint4*>(q + (8 * n + oct) * a.sq.h + 32 * i) : make_uint4(0, 0, 0, 0);
     const uint16_t* const kp = a.k + b * a.sk.b + kv * a.sk.h + 8 * quad;
     const uint16_t* const vp = a.v + b * a.sv.b + kv * a.sv.h + 8 * oct;
 
-    uint4 kr[2][D / 32];
+    uint4 kr[2][D / 32];  // keys oct and oct + 8 of the next sixteen
     auto load_k = [&](int e) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -79,8 +85,11 @@ __global__ void __launch_bounds__(kThreads) window_decode_kernel(const __grid_co
                 kr[j][i] = x < e1 ? __ldcs(reinterpret_cast<const uint4*>(kp + keys.token(x) * a.sk.t + 32 * i)) : make_uint4(0, 0, 0, 0);
         }
     };
-    float o[D / 64][8][4] = {};
-    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;  // l: this lane's keys only
+    // o: dimensions 64 i + 8 oct + 2 t (+ 1: the second half) of heads 8 n + 2 quad and + 1; m, l: of the same two heads
+    float o[kCols][D / 64][4][4] = {};
+    float m[kCols][2], l[kCols][2];  // l: this lane's keys only
+#pragma unroll
+    for (int n = 0; n < kCols; ++n) m[n][0] = m[n][1] = -INFINITY, l[n][0] = l[n][1] = 0.f;
     int e = e0 + warp * kTile;
     if (e < e1) load_k(e);
     for (; e < e1; e += kWarps * kTile) {
@@ -93,142 +102,137 @@ __global__ void __launch_bounds__(kThreads) window_decode_kernel(const __grid_co
             for (int i = 0; i < D / 64; ++i)
                 vr[y][i] = x < e1 ? __ldcs(reinterpret_cast<const uint4*>(vp + keys.token(x) * a.sv.t + 64 * i)) : make_uint4(0, 0, 0, 0);
         }
-        float s[2][4] = {};
+        float s[kCols][4] = {};  // keys oct (0, 1) and oct + 8 (2, 3), heads 2 quad and 2 quad + 1
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                mma_16816(s[j], qa[i][0], qb[i][0], qa[i][1], qb[i][1], kr[j][i].x, kr[j][i].y);
-                mma_16816(s[j], qa[i][2], qb[i][2], qa[i][3], qb[i][3], kr[j][i].z, kr[j][i].w);
+            for (int n = 0; n < kCols; ++n) {
+                mma_16816(s[n], kr[0][i].x, kr[1][i].x, kr[0][i].y, kr[1][i].y, qr[n][i].x, qr[n][i].y);
+                mma_16816(s[n], kr[0][i].z, kr[1][i].z, kr[0][i].w, kr[1][i].w, qr[n][i].z, qr[n][i].w);
             }
         if (e + kWarps * kTile < e1) load_k(e + kWarps * kTile);
-        // base-2 logarithms of the weights; keys past the run weigh nothing
-        float t0 = -INFINITY, t1 = -INFINITY;
+        uint32_t hi[kCols][2], lo[kCols][2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int n = 0; n < kCols; ++n) {
+            // base-2 logarithms of the weights; keys past the run weigh nothing
+            float t[2];
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-                s[j][y] = e + 8 * j + 2 * quad + (y & 1) < e1 ? s[j][y] * a.scale_log2 : -INFINITY;
-                if (y < 2) t0 = fmaxf(t0, s[j][y]);
-                else if (kWide) t1 = fmaxf(t1, s[j][y]);
+            for (int y = 0; y < 4; ++y) s[n][y] = e + oct + 8 * (y >> 1) < e1 ? s[n][y] * a.scale_log2 : -INFINITY;
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+                t[z] = fmaxf(s[n][z], s[n][z + 2]);
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) t[z] = fmaxf(t[z], __shfl_xor_sync(0xffffffffu, t[z], x));
+                t[z] = fmaxf(t[z], m[n][z]);
             }
+            if (__any_sync(0xffffffffu, t[0] > m[n][0] || t[1] > m[n][1])) {
 #pragma unroll
-        for (int x = 1; x < 4; x <<= 1) {
-            t0 = fmaxf(t0, __shfl_xor_sync(0xffffffffu, t0, x));
-            if (kWide) t1 = fmaxf(t1, __shfl_xor_sync(0xffffffffu, t1, x));
-        }
-        t0 = fmaxf(t0, m0), t1 = fmaxf(t1, m1);
-        if (__any_sync(0xffffffffu, t0 > m0 || t1 > m1)) {
-            const float f0 = t0 > m0 ? ex2_approx(m0 - t0) : 1.f, f1 = t1 > m1 ? ex2_approx(m1 - t1) : 1.f;
-            m0 = t0, m1 = t1;
-            l0 *= f0, l1 *= f1;
+                for (int z = 0; z < 2; ++z) {
+                    const float f = t[z] > m[n][z] ? ex2_approx(m[n][z] - t[z]) : 1.f;
+                    m[n][z] = t[z];
+                    l[n][z] *= f;
 #pragma unroll
-            for (int i = 0; i < D / 64; ++i)
+                    for (int i = 0; i < D / 64; ++i)
 #pragma unroll
-                for (int t = 0; t < 8; ++t) {
-                    o[i][t][0] *= f0, o[i][t][1] *= f0;
-                    if (kWide) o[i][t][2] *= f1, o[i][t][3] *= f1;
+                        for (int w = 0; w < 4; ++w) o[n][i][w][z] *= f, o[n][i][w][z + 2] *= f;
                 }
-        }
-        const float r0 = m0 == -INFINITY ? 0.f : m0, r1 = m1 == -INFINITY ? 0.f : m1;
-        uint32_t hi[4], lo[4];
+            }
+            const float r0 = m[n][0] == -INFINITY ? 0.f : m[n][0], r1 = m[n][1] == -INFINITY ? 0.f : m[n][1];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const float p0 = ex2_approx(s[j][0] - r0), p1 = ex2_approx(s[j][1] - r0);
-            l0 += p0 + p1;
-            split_pair(p0, p1, hi[2 * j], lo[2 * j]);
-            hi[2 * j + 1] = lo[2 * j + 1] = 0u;
-            if (kWide) {
-                const float p2 = ex2_approx(s[j][2] - r1), p3 = ex2_approx(s[j][3] - r1);
-                l1 += p2 + p3;
-                split_pair(p2, p3, hi[2 * j + 1], lo[2 * j + 1]);
+            for (int j = 0; j < 2; ++j) {
+                const float p0 = ex2_approx(s[n][2 * j] - r0), p1 = ex2_approx(s[n][2 * j + 1] - r1);
+                l[n][0] += p0;
+                l[n][1] += p1;
+                split_pair(p0, p1, hi[n][j], lo[n][j]);
+                hi[n][j] = transpose_8x8(hi[n][j]);
+                lo[n][j] = transpose_8x8(lo[n][j]);
             }
         }
 #pragma unroll
         for (int i = 0; i < D / 64; ++i)
 #pragma unroll
-            for (int t = 0; t < 8; ++t) {
-                const int w = t >> 1;
-                const uint32_t sel = (t & 1) ? 0x7632u : 0x5410u;
+            for (int w = 0; w < 4; ++w) {
                 auto word = [&](int y) { return w == 0 ? vr[y][i].x : w == 1 ? vr[y][i].y : w == 2 ? vr[y][i].z : vr[y][i].w; };
-                const uint32_t b0 = __byte_perm(word(0), word(1), sel), b1 = __byte_perm(word(2), word(3), sel);
-                mma_16816(o[i][t], hi[0], hi[1], hi[2], hi[3], b0, b1);
-                mma_16816(o[i][t], lo[0], lo[1], lo[2], lo[3], b0, b1);
-            }
-    }
+                const uint32_t a0 = __byte_perm(word(0), word(1), 0x5410u), a1 = __byte_perm(word(0), word(1), 0x7632u);
+                const uint32_t a2 = __byte_perm(word(2), word(3), 0x5410u), a3 = __byte_perm(word(2), word(3), 0x7632u);
 #pragma unroll
-    for (int x = 1; x < 4; x <<= 1) {
-        l0 += __shfl_xor_sync(0xffffffffu, l0, x);
-        l1 += __shfl_xor_sync(0xffffffffu, l1, x);
+                for (int n = 0; n < kCols; ++n) {
+                    mma_16816(o[n][i][w], a0, a1, a2, a3, hi[n][0], hi[n][1]);
+                    mma_16816(o[n][i][w], a0, a1, a2, a3, lo[n][0], lo[n][1]);
+                }
+            }
     }
 
     // ---- the four warps' parts of a row
-    if (quad == 0) {
-        s_m[warp][oct] = m0, s_l[warp][oct] = l0;
-        s_m[warp][oct + 8] = m1, s_l[warp][oct + 8] = l1;
-    }
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i)
+    for (int n = 0; n < kCols; ++n)
 #pragma unroll
-        for (int z = 0; z < (kWide ? 4 : 2); ++z)  // columns 2 quad + (z & 1) are dimensions 64 i + 8 * column + 0..7
+        for (int z = 0; z < 2; ++z) {
 #pragma unroll
-            for (int t = 0; t < 8; t += 4)
-                *reinterpret_cast<float4*>(&s_o[warp][oct + 8 * (z >> 1)][64 * i + 16 * quad + 8 * (z & 1) + t]) =
-                    make_float4(o[i][t][z], o[i][t + 1][z], o[i][t + 2][z], o[i][t + 3][z]);
+            for (int x = 4; x < 32; x <<= 1) l[n][z] += __shfl_xor_sync(0xffffffffu, l[n][z], x);
+            const int r = 8 * n + 2 * quad + z;
+            if (oct == 0) s_m[warp][r] = m[n][z], s_l[warp][r] = l[n][z];
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i)
+#pragma unroll
+                for (int w = 0; w < 4; w += 2)
+                    *reinterpret_cast<float4*>(&s_o[warp][r][64 * i + 8 * oct + 2 * w]) =
+                        make_float4(o[n][i][w][z], o[n][i][w][z + 2], o[n][i][w + 1][z], o[n][i][w + 1][z + 2]);
+        }
     __syncthreads();
     for (int x = threadIdx.x; x < rows * (D / 4); x += kThreads) {
         const int r = x / (D / 4), d = x % (D / 4) * 4;
-        float m = s_m[0][r];
+        float top = s_m[0][r];
 #pragma unroll
-        for (int w = 1; w < kWarps; ++w) m = fmaxf(m, s_m[w][r]);
-        float l = 0.f;
+        for (int w = 1; w < kWarps; ++w) top = fmaxf(top, s_m[w][r]);
+        float sum_l = 0.f;
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-            const float f = s_m[w][r] == -INFINITY ? 0.f : ex2_approx(s_m[w][r] - m);
+            const float f = s_m[w][r] == -INFINITY ? 0.f : ex2_approx(s_m[w][r] - top);
             const float4 v = *reinterpret_cast<const float4*>(&s_o[w][r][d]);
-            l += f * s_l[w][r];
+            sum_l += f * s_l[w][r];
             sum.x += f * v.x, sum.y += f * v.y, sum.z += f * v.z, sum.w += f * v.w;
         }
         const long long row = static_cast<long long>(b) * a.H + h0 + r;
         if (a.splits == 1) {
-            const float inv = keys.n > 0 ? 1.f / l : 0.f;
+            const float inv = keys.n > 0 ? 1.f / sum_l : 0.f;
             *reinterpret_cast<uint2*>(a.o + b * a.so.b + (h0 + r) * a.so.h + d) =
                 make_uint2(pack_bf16x2(sum.x * inv, sum.y * inv), pack_bf16x2(sum.z * inv, sum.w * inv));
-            if (d == 0) a.lse[row] = keys.n > 0 ? (m + log2f(l)) * kLn2 : -INFINITY;
+            if (d == 0) a.lse[row] = keys.n > 0 ? (top + log2f(sum_l)) * kLn2 : -INFINITY;
         } else {
             const long long at = row * a.splits + split;
             *reinterpret_cast<float4*>(a.part_o + at * D + d) = sum;
-            if (d == 0) a.part_ml[at] = make_float2(m, l);
+            if (d == 0) a.part_ml[at] = make_float2(top, sum_l);
         }
     }
 }
 
-// Joins the runs of a row (a block): its warps take runs in turn, a lane D/32 dimensions.
-template <int D>
-__global__ void __launch_bounds__(256) window_join_kernel(const __grid_constant__ DecodeArgs a) {
-    constexpr int kPer = D / 32, kJoinWarps = 8;
-    __shared__ float s_o[kJoinWarps][D];
-    __shared__ float2 s_ml[kJoinWarps];
+// Joins the runs of a row: kPer warps to a row take its runs in turn, a lane D/32 dimensions; 8 / kPer rows (kPer <= 8) to a block.
+template <int D, int kPer>
+__global__ void __launch_bounds__(kPer > 8 ? 32 * kPer : 256) window_join_kernel(const __grid_constant__ DecodeArgs a, int n_rows) {
+    constexpr int kDims = D / 32, kBlockWarps = kPer > 8 ? kPer : 8, kBlockRows = kBlockWarps / kPer;
+    __shared__ float s_o[kPer > 1 ? kBlockWarps : 1][D];
+    __shared__ float2 s_ml[kBlockWarps];
     griddep_launch_dependents();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % kPer;
+    const int row = static_cast<int>(blockIdx.x) * kBlockRows + warp / kPer, b = min(row, n_rows - 1) / a.H, h = row - b * a.H;
     griddep_wait();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int b = blockIdx.x / a.H, h = blockIdx.x - b * a.H;
     const DecodeKeys keys = decode_keys(a, __ldg(a.lengths + b));
-    const int runs = (keys.n + a.chunk - 1) / a.chunk;
-    const long long at = static_cast<long long>(blockIdx.x) * a.splits;
-    float m = -INFINITY, l = 0.f, o[kPer] = {};
-    constexpr int kDeep = 4;
-    for (int s = warp; s < runs; s += kJoinWarps * kDeep) {
+    const int runs = row < n_rows ? (keys.n + a.chunk - 1) / a.chunk : 0;
+    const long long at = static_cast<long long>(row) * a.splits;
+    float m = -INFINITY, l = 0.f, o[kDims] = {};
+    constexpr int kDeep = 8;
+    for (int s = part; s < runs; s += kPer * kDeep) {
         float2 ml[kDeep];
-        float v[kDeep][kPer];
+        float v[kDeep][kDims];
 #pragma unroll
         for (int x = 0; x < kDeep; ++x) {
-            const int run = s + x * kJoinWarps;
+            const int run = s + x * kPer;
             ml[x] = make_float2(-INFINITY, 0.f);
             if (run < runs) ml[x] = a.part_ml[at + run];
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) v[x][i] = run < runs ? a.part_o[(at + run) * D + lane * kPer + i] : 0.f;
+            for (int i = 0; i < kDims; ++i) v[x][i] = run < runs ? a.part_o[(at + run) * D + lane * kDims + i] : 0.f;
         }
 #pragma unroll
         for (int x = 0; x < kDeep; ++x) {
@@ -237,29 +241,38 @@ __global__ void __launch_bounds__(256) window_join_kernel(const __grid_constant_
             m = t;
             l = l * f + ml[x].y * w;
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) o[i] = o[i] * f + v[x][i] * w;
+            for (int i = 0; i < kDims; ++i) o[i] = o[i] * f + v[x][i] * w;
         }
     }
-    if (lane == 0) s_ml[warp] = make_float2(m, l);
+    if constexpr (kPer > 1) {
+        if (lane == 0) s_ml[warp] = make_float2(m, l);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) s_o[warp][lane * kPer + i] = o[i];
-    __syncthreads();
-    if (threadIdx.x >= D / 2) return;
-    float top = -INFINITY;
+        for (int i = 0; i < kDims; ++i) s_o[warp][lane * kDims + i] = o[i];
+        __syncthreads();
+        if (part != 0) return;
+        float top = -INFINITY;
+        for (int w = 0; w < kPer; ++w) top = fmaxf(top, s_ml[warp + w].x);
+        const float r = top == -INFINITY ? 0.f : top;
+        m = top;
+        l = 0.f;
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) top = fmaxf(top, s_ml[w].x);
-    const float r = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, x0 = 0.f, x1 = 0.f;
+        for (int i = 0; i < kDims; ++i) o[i] = 0.f;
+#pragma unroll 8
+        for (int w = 0; w < kPer; ++w) {
+            const float f = ex2_approx(s_ml[warp + w].x - r);
+            l += f * s_ml[warp + w].y;
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) {
-        const float f = ex2_approx(s_ml[w].x - r);
-        sum += f * s_ml[w].y;
-        x0 += f * s_o[w][2 * threadIdx.x];
-        x1 += f * s_o[w][2 * threadIdx.x + 1];
+            for (int i = 0; i < kDims; ++i) o[i] += f * s_o[warp + w][lane * kDims + i];
+        }
     }
-    const float inv = keys.n > 0 ? 1.f / sum : 0.f;
-    *reinterpret_cast<uint32_t*>(a.o + b * a.so.b + h * a.so.h + 2 * threadIdx.x) = pack_bf16x2(x0 * inv, x1 * inv);
-    if (threadIdx.x == 0) a.lse[blockIdx.x] = keys.n > 0 ? (top + log2f(sum)) * kLn2 : -INFINITY;
+    if (row >= n_rows) return;
+    const float inv = keys.n > 0 ? 1.f / l : 0.f;
+    uint16_t* const to = a.o + b * a.so.b + h * a.so.h + lane * kDims;
+    if constexpr (kDims == 2)
+        *reinterpret_cast<uint32_t*>(to) = pack_bf16x2(o[0] * inv, o[1] * inv);
+    else
+        *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv));
+    if (lane == 0) a.lse[row] = keys.n > 0 ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
 }  // namespace
@@ -283,14 +296,19 @@ DecodePlan decode_plan(int B, int H, int H_kv, int T_max, int window, int sinks)
 cudaError_t launch_window_decode(const DecodeArgs& a, int D, long long items, int B, cudaStream_t stream) {
     const dim3 grid(static_cast<unsigned>(items * a.splits));
     auto go = [&](auto kernel) { return launch_overlapped(kernel, grid, dim3(kThreads), 0, stream, a); };
-    const bool wide = a.group > 8;
-    const cudaError_t e = D == 64 ? (wide ? go(window_decode_kernel<64, true>) : go(window_decode_kernel<64, false>))
-                                  : (wide ? go(window_decode_kernel<128, true>) : go(window_decode_kernel<128, false>));
+    const bool two = a.group > 8;
+    const cudaError_t e = D == 64 ? (two ? go(window_decode_kernel<64, 2>) : go(window_decode_kernel<64, 1>))
+                                  : (two ? go(window_decode_kernel<128, 2>) : go(window_decode_kernel<128, 1>));
     if (e != cudaSuccess || a.splits == 1) return e;
-    auto join = [&](auto kernel) {
-        return launch_overlapped(kernel, dim3(static_cast<unsigned>(B) * a.H), dim3(256), 0, stream, a);
+    // Warps to a row: all of its runs in flight at once.
+    const int n_rows = B * a.H;
+    auto join = [&](auto kernel, int per) {
+        const int rows = per > 8 ? 1 : 8 / per;
+        return launch_overlapped(kernel, dim3((n_rows + rows - 1) / rows), dim3(per > 8 ? 32 * per : 256), 0, stream, a, n_rows);
     };
-    return D == 64 ? join(window_join_kernel<64>) : join(window_join_kernel<128>);
+    if (a.splits <= 8) return D == 64 ? join(window_join_kernel<64, 1>, 1) : join(window_join_kernel<128, 1>, 1);
+    if (a.splits <= 64) return D == 64 ? join(window_join_kernel<64, 8>, 8) : join(window_join_kernel<128, 8>, 8);
+    return D == 64 ? join(window_join_kernel<64, 32>, 32) : join(window_join_kernel<128, 32>, 32);
 }
 
 }  // namespace nova
