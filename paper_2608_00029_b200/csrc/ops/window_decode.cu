@@ -3,7 +3,7 @@
 // Memory bound: every kept key and value is read once, 4*D bytes, for the G query heads that share it.  A CTA takes a run of
 // `chunk` kept keys of one key/value head of one sequence (so that sequences of all lengths make CTAs of one size), its four
 // warps every fourth 16 of them; what a CTA finds, its maximum, sum and weighted sum per query head, is joined with the
-// other runs' by a second kernel unless one run holds all.
+// other runs' by a second kernel, or where there are few CTAs and a row's runs fit a cluster by these CTAs themselves.
 //
 // The two products go through the warp-level tensor instruction (m16n8k16), keys or dimensions as its 16 rows, query heads as its 8
 // columns: not for its rate, of which they need a tenth, but because the dot products of G heads with one key would otherwise be
@@ -47,12 +47,34 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
     return y;
 }
 
-// kCols: groups of 8 query heads.
-template <int D, int kCols>
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The same shared-memory address in the CTA of the cluster with number `rank`.
+__device__ __forceinline__ uint32_t peer_address(const void* p, int rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float4 load_peer4(uint32_t at) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 load_peer2(uint32_t at) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(at) : "memory");
+    return v;
+}
+
+// kCols: groups of 8 query heads.  kCluster: the runs of a row are a cluster (no CTA leaves before the others have read from it).
+template <int D, int kCols, bool kCluster>
 __global__ void __launch_bounds__(kThreads, kCols == 1 ? (D == 64 ? 5 : 3) : (D == 64 ? 3 : 2))
 window_decode_kernel(const __grid_constant__ DecodeArgs a) {
     __shared__ float s_o[kWarps][8 * kCols][D + 4];  // (rows of a warp's eight lanes in different banks)
     __shared__ float s_m[kWarps][8 * kCols], s_l[kWarps][8 * kCols];
+    __shared__ float4 s_run[kCluster ? 8 * kCols : 1][D / 4];  // kCluster: the CTA's sums, and their maxima and weights
+    __shared__ float2 s_run_ml[8 * kCols];
     griddep_launch_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = lane & 3, oct = lane >> 2;
     const int item = blockIdx.x / a.splits, split = blockIdx.x - item * a.splits;
@@ -62,7 +84,7 @@ window_decode_kernel(const __grid_constant__ DecodeArgs a) {
     griddep_wait();
     const DecodeKeys keys = decode_keys(a, __ldg(a.lengths + b));
     const int e0 = split * a.chunk, e1 = min(keys.n, e0 + a.chunk);
-    if (e0 >= e1 && !(split == 0 && a.splits == 1)) return;  // (a run that is not there is not looked for either)
+    if (!kCluster && e0 >= e1 && !(split == 0 && a.splits == 1)) return;  // (a run that is not there is not looked for either)
 
     // Q^T as the second operand: column oct of each group of heads
     uint4 qr[kCols][D / 32];
@@ -195,7 +217,10 @@ window_decode_kernel(const __grid_constant__ DecodeArgs a) {
             sum.x += f * v.x, sum.y += f * v.y, sum.z += f * v.z, sum.w += f * v.w;
         }
         const long long row = static_cast<long long>(b) * a.H + h0 + r;
-        if (a.splits == 1) {
+        if (kCluster) {
+            s_run[r][d / 4] = sum;
+            if (d == 0) s_run_ml[r] = make_float2(top, sum_l);
+        } else if (a.splits == 1) {
             const float inv = keys.n > 0 ? 1.f / sum_l : 0.f;
             *reinterpret_cast<uint2*>(a.o + b * a.so.b + (h0 + r) * a.so.h + d) =
                 make_uint2(pack_bf16x2(sum.x * inv, sum.y * inv), pack_bf16x2(sum.z * inv, sum.w * inv));
@@ -205,6 +230,40 @@ window_decode_kernel(const __grid_constant__ DecodeArgs a) {
             *reinterpret_cast<float4*>(a.part_o + at * D + d) = sum;
             if (d == 0) a.part_ml[at] = make_float2(top, sum_l);
         }
+    }
+    if constexpr (kCluster) {  // the CTAs share the row's columns
+        cluster_sync();
+        for (int x = split * kThreads + threadIdx.x; x < rows * (D / 4); x += a.splits * kThreads) {
+            const int r = x / (D / 4), d = x % (D / 4) * 4;
+            float2 ml[8];
+            float4 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                ml[k] = make_float2(-INFINITY, 0.f);
+                v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (k < a.splits) {
+                    ml[k] = load_peer2(peer_address(&s_run_ml[r], k));
+                    v[k] = load_peer4(peer_address(&s_run[r][d / 4], k));
+                }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) top = fmaxf(top, ml[k].x);
+            float sum_l = 0.f;
+            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (k >= a.splits) break;
+                const float f = ml[k].x == -INFINITY ? 0.f : ex2_approx(ml[k].x - top);
+                sum_l += f * ml[k].y;
+                sum.x += f * v[k].x, sum.y += f * v[k].y, sum.z += f * v[k].z, sum.w += f * v[k].w;
+            }
+            const float inv = keys.n > 0 ? 1.f / sum_l : 0.f;
+            *reinterpret_cast<uint2*>(a.o + b * a.so.b + (h0 + r) * a.so.h + d) =
+                make_uint2(pack_bf16x2(sum.x * inv, sum.y * inv), pack_bf16x2(sum.z * inv, sum.w * inv));
+            if (d == 0) a.lse[static_cast<long long>(b) * a.H + h0 + r] = keys.n > 0 ? (top + log2f(sum_l)) * kLn2 : -INFINITY;
+        }
+        cluster_sync();
     }
 }
 
@@ -297,8 +356,27 @@ cudaError_t launch_window_decode(const DecodeArgs& a, int D, long long items, in
     const dim3 grid(static_cast<unsigned>(items * a.splits));
     auto go = [&](auto kernel) { return launch_overlapped(kernel, grid, dim3(kThreads), 0, stream, a); };
     const bool two = a.group > 8;
-    const cudaError_t e = D == 64 ? (two ? go(window_decode_kernel<64, 2>) : go(window_decode_kernel<64, 1>))
-                                  : (two ? go(window_decode_kernel<128, 2>) : go(window_decode_kernel<128, 1>));
+    // A cluster holds its SMs until its longest run is through, which does not matter where there are SMs for all.
+    if (a.splits > 1 && a.splits <= 8 && items * a.splits <= 2 * 148) {
+        auto together = [&](auto kernel) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = grid;
+            cfg.blockDim = dim3(kThreads);
+            cfg.stream = stream;
+            cudaLaunchAttribute attr[2];
+            attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr[0].val.programmaticStreamSerializationAllowed = 1;
+            attr[1].id = cudaLaunchAttributeClusterDimension;
+            attr[1].val.clusterDim = {static_cast<unsigned>(a.splits), 1, 1};
+            cfg.attrs = attr;
+            cfg.numAttrs = 2;
+            return cudaLaunchKernelEx(&cfg, kernel, a);
+        };
+        return D == 64 ? (two ? together(window_decode_kernel<64, 2, true>) : together(window_decode_kernel<64, 1, true>))
+                       : (two ? together(window_decode_kernel<128, 2, true>) : together(window_decode_kernel<128, 1, true>));
+    }
+    const cudaError_t e = D == 64 ? (two ? go(window_decode_kernel<64, 2, false>) : go(window_decode_kernel<64, 1, false>))
+                                  : (two ? go(window_decode_kernel<128, 2, false>) : go(window_decode_kernel<128, 1, false>));
     if (e != cudaSuccess || a.splits == 1) return e;
     // Warps to a row: all of its runs in flight at once.
     const int n_rows = B * a.H;
