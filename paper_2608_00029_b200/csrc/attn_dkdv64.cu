@@ -498,17 +498,24 @@ __device__ __forceinline__ void kv64_edges(uint8_t* smem, Kv64Bars* bars, uint32
         }
         return true;
     };
-    // Row terms of the item's steps in [from, to) that are this warp's; g0: steps of all items before this one.
-    auto rows = [&](int bh, int s0, int g0, int from, int to) -> bool {
-        const size_t base = static_cast<size_t>(bh) * wk.T;
+    // Row terms of the item's steps in [from, to) that are this warp's; g0: steps of all items before this one.  kWindow: the item
+    // begins at step `off` of its tile's list, of which a query head has `per`.
+    auto rows = [&](int bh, int s0, int off, int per, int g0, int from, int to) -> bool {
+        size_t base = static_cast<size_t>(bh) * wk.T;
         uint8_t* const row = smem + kOffExt + (lane >> 3) * 2 * kExtCore + (lane & 7) * 16;
         constexpr int kNext32 = 32 / 8 * 2 * kExtCore;  // the row 32 queries on
         for (int s = from + ((ow - g0 - from) & 3); s < to; s += 4) {
             const int g = g0 + s, st = g % kQStages;
+            int sh = s;  // the step in its query head
+            if constexpr (kWindow) {
+                const int head = (off + s) / per;
+                sh = off + s - head * per;
+                base = (static_cast<size_t>(bh) * wk.win.group + head) * wk.T;
+            }
             RowTerms t[2];
 #pragma unroll
             for (int x = 0; x < 2; ++x) {  // (past L1: there was no griddep_wait)
-                const int q = (s0 + s) * kStep + lane + 32 * x;
+                const int q = (s0 + sh) * kStep + lane + 32 * x;
                 t[x] = row_terms((q < wk.T) ? -__ldcg(LSE + base + q) * inv_scale : -kMostLse,
                                  (q < wk.T) ? -__ldcg(Delta + base + q) : 0.f);
             }
@@ -616,12 +623,13 @@ __device__ __forceinline__ void kv64_edges(uint8_t* smem, Kv64Bars* bars, uint32
         }
         int kt, bh, s0, n;
         wk.get(item, &kt, &bh, &s0, &n);
-        if (!kTerms) ok = rows(bh, s0, g0, 0, min(n, 2));
+        const int off = kWindow ? wk.offset(item) : 0, per = wk.per_head(kt, n);
+        if (!kTerms) ok = rows(bh, s0, off, per, g0, 0, min(n, 2));
         if (ok) ok = operand(w, 0);
         if (ok) ok = operand(w, 1);
-        if (ok && !kTerms) ok = rows(bh, s0, g0, 2, min(n, kQStages));
+        if (ok && !kTerms) ok = rows(bh, s0, off, per, g0, 2, min(n, kQStages));
         if (ok && w > 0) ok = write_out(w - 1, kt_out, bh_out, slot_out);
-        if (ok && !kTerms) ok = rows(bh, s0, g0, kQStages, n);
+        if (ok && !kTerms) ok = rows(bh, s0, off, per, g0, kQStages, n);
         kt_out = kt;
         bh_out = bh;
         slot_out = wk.slot(item);
@@ -638,7 +646,7 @@ attn_dkdv64_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                    const float* __restrict__ LSE, const float* __restrict__ Delta, const uint8_t* __restrict__ terms, int T, int BH,
                    int H, uint32_t orders, float scale, int* __restrict__ dev_status, const Window win, const KvParts parts,
                    float* __restrict__ partial) {
-    static_assert(!kWindow || (kCausal && kTerms), "with the window the row terms are prepared");
+    static_assert(!kWindow || (kCausal && !kTerms), "with the window the kernel makes the row terms itself");
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     Kv64Bars* bars = reinterpret_cast<Kv64Bars*>(smem + kOffBar);
@@ -736,8 +744,8 @@ cudaError_t configure_attn_dkdv64() {
     if (e == cudaSuccess) e = set(attn_dkdv64_kernel<true, true, true, false>);
     if (e == cudaSuccess) e = set(attn_dkdv64_kernel<false, false, true, false>);
     if (e == cudaSuccess) e = set(attn_dkdv64_kernel<false, true, true, false>);
-    if (e == cudaSuccess) e = set(attn_dkdv64_kernel<true, false, true, true>);
-    if (e == cudaSuccess) e = set(attn_dkdv64_kernel<true, true, true, true>);
+    if (e == cudaSuccess) e = set(attn_dkdv64_kernel<true, false, false, true>);
+    if (e == cudaSuccess) e = set(attn_dkdv64_kernel<true, true, false, true>);
     return e;
 }
 
@@ -768,15 +776,15 @@ cudaError_t launch_attn_dkdv64(const CUtensorMap& tmQ, const CUtensorMap& tmK, c
 
 cudaError_t launch_window_dkdv64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
                                  const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided, uint32_t orders, const float* LSE,
-                                 const float* Delta, const void* terms, const AttnShape& s, const Window& win, const KvParts& parts,
-                                 float* partial, int* dev_status, cudaStream_t stream) {
+                                 const float* Delta, const AttnShape& s, const Window& win, const KvParts& parts, float* partial,
+                                  int* dev_status, cudaStream_t stream) {
     const int H = s.H / win.group, BH = s.B * H;
     const dim3 grid(static_cast<unsigned>(parts.items(BH)));
     auto go = [&](auto kernel) {
         return launch_overlapped(kernel, grid, dim3(kThreads), kSmemBytes, stream, tmQ, tmK, tmV, tmdO, tmdK, tmdV, LSE, Delta,
-                                 static_cast<const uint8_t*>(terms), s.T, BH, H, orders, s.scale, dev_status, win, parts, partial);
+                                 nullptr, s.T, BH, H, orders, s.scale, dev_status, win, parts, partial);
     };
-    return strided ? go(attn_dkdv64_kernel<true, true, true, true>) : go(attn_dkdv64_kernel<true, false, true, true>);
+    return strided ? go(attn_dkdv64_kernel<true, true, false, true>) : go(attn_dkdv64_kernel<true, false, false, true>);
 }
 
 }  // namespace nova

@@ -220,8 +220,8 @@ cudaError_t launch_attn_dkdv64(const CUtensorMap& tmQ, const CUtensorMap& tmK, c
                                int* dev_status, cudaStream_t stream);
 cudaError_t launch_window_dkdv64(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
                                  const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided, uint32_t orders, const float* LSE,
-                                 const float* Delta, const void* terms, const AttnShape& s, const Window& win, const KvParts& parts,
-                                 float* partial, int* dev_status, cudaStream_t stream);
+                                 const float* Delta, const AttnShape& s, const Window& win, const KvParts& parts, float* partial,
+                                 int* dev_status, cudaStream_t stream);
 cudaError_t configure_attn_dkdv64();
 
 // Heads that the items of the kernels at D=128 are taken in together: enough items for two rounds of the SMs, and no more

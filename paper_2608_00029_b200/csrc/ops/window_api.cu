@@ -24,14 +24,9 @@ size_t decode_bytes(const DecodePlan& p, int B, int H, int D) {
 
 Window window_of(int H, int H_kv, int T, int window, int sinks) { return Window{std::min(window, T), std::min(sinks, T), H / H_kv}; }
 
-// The row terms of the dK/dV kernel at D = 64 (32 bytes a row, the rows of a head rounded up to kKeyStep), then the slots of the key
-// tiles that are summed in parts.
-size_t terms_bytes(int B, int H, int T, int D) {
-    return D == 64 ? static_cast<size_t>(B) * H * ((T + kKeyStep - 1) / kKeyStep) * kKeyStep * 32 : 0;
-}
-size_t bwd_bytes(int B, int H, int H_kv, int T, int D, const KvParts& parts) {
-    const size_t slots = static_cast<size_t>(parts.slots(static_cast<long long>(B) * H_kv)) * 2 * kBlockK * D * sizeof(float);
-    return std::max<size_t>(256, terms_bytes(B, H, T, D) + slots);
+// The slots of the key tiles that are summed in parts.
+size_t bwd_bytes(int B, int H_kv, int D, const KvParts& parts) {
+    return std::max<size_t>(256, static_cast<size_t>(parts.slots(static_cast<long long>(B) * H_kv)) * 2 * kBlockK * D * sizeof(float));
 }
 
 }  // namespace
@@ -86,7 +81,7 @@ int nova_window_bwd_preprocess(const void* O, const void* O_rest, const void* dO
 
 size_t nova_window_bwd_workspace_bytes(int B, int H, int H_kv, int T, int D, int window, int sinks) {
     if (check_window(B, H, H_kv, T, D, window, sinks) != NOVA_ATTN_OK) return 0;
-    return bwd_bytes(B, H, H_kv, T, D, kv_parts(B * H_kv, T, window_of(H, H_kv, T, window, sinks)));
+    return bwd_bytes(B, H_kv, D, kv_parts(B * H_kv, T, window_of(H, H_kv, T, window, sinks)));
 }
 
 int nova_window_bwd(const void* Q, const void* K, const void* V, const void* dO, const float* LSE, const float* Delta, void* dQ, void* dK,
@@ -106,7 +101,7 @@ int nova_window_bwd(const void* Q, const void* K, const void* V, const void* dO,
     if (int rc = check_strides(dv_strides, D, &sdv)) return rc;
     const Window win = window_of(H, H_kv, T, window, sinks);
     const KvParts parts = kv_parts(B * H_kv, T, win);
-    if (!workspace || workspace_bytes < bwd_bytes(B, H, H_kv, T, D, parts)) return NOVA_ATTN_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < bwd_bytes(B, H_kv, D, parts)) return NOVA_ATTN_ERR_WORKSPACE;
     if (parts.items(static_cast<long long>(B) * H_kv) > 0x7fffffffll) return NOVA_ATTN_ERR_SHAPE;
     if (!aligned16(workspace)) return NOVA_ATTN_ERR_ALIGNMENT;
     DeviceState* st = nullptr;
@@ -131,15 +126,13 @@ int nova_window_bwd(const void* Q, const void* K, const void* V, const void* dO,
     const uint32_t orders = oq | (ok << 4) | (ov << 8) | (odo << 12);
     const uint32_t orders_dq = orders | (odq << 16), orders_kv = orders | (odk << 16) | (odv << 20);
     const cudaStream_t cs = static_cast<cudaStream_t>(stream);
-    float* const partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + terms_bytes(B, H, T, D));
+    float* const partial = static_cast<float*>(workspace);
     cudaError_t e;
     if (D == 64) {
-        e = launch_row_terms64(LSE, Delta, workspace, s, cs);
+        e = launch_window_dq64(tmQ, tmKs, tmVs, tmdO, tmdQ, strided, orders_dq, LSE, Delta, s, win, st->dev_status, cs);
         if (e == cudaSuccess)
-            e = launch_window_dq64(tmQ, tmKs, tmVs, tmdO, tmdQ, strided, orders_dq, LSE, Delta, s, win, st->dev_status, cs);
-        if (e == cudaSuccess)
-            e = launch_window_dkdv64(tmQs, tmK, tmV, tmdOs, tmdK, tmdV, strided, orders_kv, LSE, Delta, workspace, s, win, parts,
-                                     partial, st->dev_status, cs);
+            e = launch_window_dkdv64(tmQs, tmK, tmV, tmdOs, tmdK, tmdV, strided, orders_kv, LSE, Delta, s, win, parts, partial,
+                                     st->dev_status, cs);
     } else {
         e = launch_window_dq(tmQ, tmKs, tmVs, tmdO, tmdQ, strided, orders_dq, LSE, Delta, s, win, st->num_sms, st->dev_status, cs);
         if (e == cudaSuccess)

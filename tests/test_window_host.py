@@ -111,8 +111,10 @@ def test_window_calls_refuse_bad_arguments(lib):
 
 def test_workspace_queries(lib):
     from paper_2608_00029_b200 import nova_window as nw
-    assert nw.nova_window_bwd_workspace_bytes(2, 4, 2, 100, 64, 10, 1) >= 2 * 4 * 128 * 32
-    assert nw.nova_window_bwd_workspace_bytes(2, 4, 2, 100, 128, 10, 1) >= 256
+    for D in (64, 128):  # nothing in parts, and the tile of the sinks in parts
+        assert nw.nova_window_bwd_workspace_bytes(2, 4, 2, 100, D, 10, 1) == 256
+        assert nw.nova_window_bwd_workspace_bytes(1, 4, 1, 8000, D, 64, 4) % (2 * 128 * D * 4) == 0
+        assert nw.nova_window_bwd_workspace_bytes(1, 4, 1, 8000, D, 64, 4) > 2 * 128 * D * 4
     for bad in ((0, 4, 2, 100, 64, 10, 1), (2, 4, 3, 100, 64, 10, 1), (2, 4, 2, 100, 96, 10, 1), (2, 4, 2, 100, 64, 0, 1),
                 (2, 4, 2, 100, 64, 10, -1)):
         assert nw.nova_window_bwd_workspace_bytes(*bad) == 0 and nw.nova_window_decode_workspace_bytes(*bad) == 0
