@@ -66,7 +66,7 @@ __device__ __forceinline__ typename Vec<V>::type narrow(const float (&f)[V]) {
 // are V/2 pairs.  A unit is a chunk of V places (the last ones are copied), a token and a group of heads; units next to each
 // other have the chunks of one head and then, whichever lies closer, the token's other heads or the head's other tokens.
 template <int V, bool kInterleaved>
-__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeArgs a) {
+__global__ void __launch_bounds__(kThreads, 3) rope_kernel(const __grid_constant__ RopeArgs a) {
     using T4 = typename Vec<V>::type;
     constexpr int kAngles = kInterleaved ? V / 2 : V;
     constexpr int kHeadsInFlight = heads_in_flight(kInterleaved);
@@ -213,7 +213,7 @@ int rope(const void* Q, const void* K, void* Qo, void* Ko, const float* inv_freq
     const bool in_place = Q == Qo && (!K || K == Ko);
     a.chunks = a.rot_chunks + (in_place ? 0 : (D - rotary) / v);
     a.heads_inside = a.sin[0].h < a.sin[0].t;
-    // Heads in flight to a thread, if that leaves 512 threads for every SM (24 heads, R=64, half layout, B=8, T=1024: 9.7 us with
+    // Heads in flight to a thread, if that leaves 512 threads for every SM (24 heads, R=64, half layout, B=8, T=1024: 9.2 us with
     // four, 11.2 with all of them to a thread); tokens for whole blocks, if that leaves a block for every SM.
     const int heads = H + H_kv;
     a.rows = B * T;
