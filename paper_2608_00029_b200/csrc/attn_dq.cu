@@ -10,7 +10,7 @@
 // one kernel.
 //
 // A work item is a block of 256 query rows of one head: two 128-row tiles, A and B, that share every K and V tile
-// they both need; in small problems one tile (plan_of).  The keys go by in steps of 64.  Items are handed out dynamically,
+// they both need; in small problems one tile (plan_of).  With a window tile B leaves out the first keys of A's.  The keys go by in steps of 64.  Items are handed out dynamically,
 // heaviest first, as in the forward (WorkRing).  384 threads:
 //   warp 0      TMA producer: Q and dO per tile of an item, K and V through a ring of 64-key stages
 //   warps 1, 3  UMMA issuers, one per query tile, so that neither tile waits for the other's products and A may be in
@@ -87,8 +87,20 @@ struct DqWork {
     int BH, n_blocks, chunk, T, H;
     uint32_t orders;  // coordinate orders of the Q, K, V, dO, dQ tensor maps, four bits each
     bool causal;
-    Window win;  // kWindow: single tiles only
-    __device__ __forceinline__ KeySpan span(int blk) const { return key_span(win, blk * kBlockQ, kBlockQ, T, kStep); }
+    Window win;
+    // kWindow: the steps of a block.  Tile B leaves out [skip, resume) of them, what only tile A's window reaches; the last ones
+    // are beyond tile A's diagonal (its number of steps is smaller).
+    __device__ __forceinline__ KeySpan span(int blk) const { return key_span(win, blk * kTiles * kBlockQ, kTiles * kBlockQ, T, kStep); }
+    __device__ __forceinline__ void left_out(int blk, int t, int n_t, int* skip, int* resume) const {
+        *skip = *resume = n_t;
+        if (!kWindow || kTiles == 1 || t == 0 || n_t == 0) return;
+        const KeySpan s = span(blk);
+        const int first_a = blk * kTiles * kBlockQ - win.window + 1, first_b = first_a + kBlockQ;
+        const int lo_a = first_a > 0 ? first_a / kStep : 0, lo_b = first_b > 0 ? first_b / kStep : 0;
+        const int all = (win.sinks + kStep - 1) / kStep;
+        *skip = s.sinks + max(0, min(all, lo_b) - lo_a);
+        *resume = s.sinks + lo_b - lo_a;
+    }
     // Block index, head, and the number of key steps each tile visits (0: the tile lies past the end of the sequence).
     __device__ __forceinline__ void get(int idx, int* blk, int* bh, int* n_a, int* n_b) const {
         if constexpr (D == 128) {
@@ -107,8 +119,10 @@ struct DqWork {
             *bh = idx % BH;
         }
         if constexpr (kWindow) {
-            *n_a = span(*blk).n;
-            *n_b = 0;
+            const int n = span(*blk).n, row_b = (*blk * kTiles + 1) * kBlockQ;  // tile B's first row
+            const bool b = kTiles == 2 && row_b < T;
+            *n_a = b ? n - ((min(row_b + kBlockQ, T) - 1) / kStep - (row_b - 1) / kStep) : n;
+            *n_b = b ? n : 0;
             return;
         }
         const int n_all = (T + kStep - 1) / kStep;
@@ -273,65 +287,81 @@ __device__ __forceinline__ void dq_mma(uint8_t* smem, DqBars* bars, uint32_t tme
             }
         } else {
             const uint32_t t_s = t_dq + Cfg::kColS, t_dp = t_dq + Cfg::kColdP;
-            int st_n = st;  // stage of the step whose S and dP come next
-            uint32_t ph_n = ph;
-            // S and dP of the item's first step.  Their columns are free: the row warps have read the previous step's
-            // (sp_free was awaited below, or is here), and a dS that lies over S was consumed by a dQ product queued
-            // earlier.
-            if (n_t > 0) {
-                ok = mbar_wait(&bars->kv_full[st_n], ph_n, abort_flag);
-                if (ok && cq > 0) ok = mbar_wait(&bars->sp_free[0][t], (cq - 1) & 1, abort_flag);
-                if (!ok) break;
-                tc_fence_after();
-                if (el) {
-                    product(t_s, q_k, k_k0 + st_n * (Cfg::kStepBytes >> 4));
-                    product(t_dp, do_k, v_k0 + st_n * (Cfg::kStepBytes >> 4));
-                    tc_commit(&bars->sp_full[0][t]);
+            int skip, resume, done = 0;  // done: steps of the item so far
+            wk.left_out(blk, t, n_t, &skip, &resume);
+            // The steps before those left out, and those after: nothing looks ahead from the ones to the others, because their stages may
+            // be the same.
+#pragma unroll 1
+            for (int part = 0; part < (kWindow && kTiles == 2 ? 2 : 1) && ok; ++part) {
+                const int j0 = part == 0 ? 0 : resume, j1 = part == 0 ? skip : n_t;
+                for (int j = skip; part == 1 && j < resume; ++j) {  // this tile's share of their release, as below
+                    ok = mbar_wait(&bars->kv_full[st], ph, abort_flag);
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive(&bars->kv_empty[st]);
+                    __syncwarp();
+                    next_stage(&st, &ph);
                 }
-                __syncwarp();
-                ++cq;
-                next_stage(&st_n, &ph_n);
-            }
-            for (int j = 0; j < n_t; ++j, ++c) {
-                const bool more = j + 1 < n_t;
-                if (more) {  // dP (and S, where dS has columns of its own) of the next step, once this step's have been read
+                if (!ok) break;
+                int st_n = st;  // stage of the step whose S and dP come next
+                uint32_t ph_n = ph;
+                // S and dP of the first step.  Their columns are free: the row warps have read the previous step's
+                // (sp_free was awaited below, or is here), and a dS that lies over S was consumed by a dQ product queued
+                // earlier.
+                if (j0 < j1) {
                     ok = mbar_wait(&bars->kv_full[st_n], ph_n, abort_flag);
-                    if (ok) ok = mbar_wait(&bars->sp_free[0][t], (cq - 1) & 1, abort_flag);
+                    if (ok && cq > 0) ok = mbar_wait(&bars->sp_free[0][t], (cq - 1) & 1, abort_flag);
                     if (!ok) break;
                     tc_fence_after();
                     if (el) {
-                        if (Cfg::kSepdS) product(t_s, q_k, k_k0 + st_n * (Cfg::kStepBytes >> 4));
-                        product(t_dp, do_k, v_k0 + st_n * (Cfg::kStepBytes >> 4));
-                        if (Cfg::kSepdS) tc_commit(&bars->sp_full[0][t]);
-                    }
-                    __syncwarp();
-                }
-                ok = mbar_wait(&bars->ds_ready[c & 1][t], (c >> 1) & 1, abort_flag);
-                // the previous item's dQ must have been read out of TMEM before it is overwritten
-                if (ok && j == 0 && wt > 0) ok = mbar_wait(&bars->dq_free[t], (wt - 1) & 1, abort_flag);
-                if (!ok) break;
-                tc_fence_after();
-                // dQ += dS K_j: dS from TMEM (16 keys = 8 packed columns per instruction), K MN-major (rows = keys,
-                // 64 head-dim elements per 128-byte row, the second 64-wide half kHalfStepBytes further).
-                if (el) {
-                    const uint32_t t_ds = t_dq + Cfg::kColdS + (Cfg::kSepdS ? 32 * (c & 1) : 0);
-                    const uint32_t k_m = k_m0 + st * (Cfg::kStepBytes >> 4);
-#pragma unroll
-                    for (int k = 0; k < kStep / 16; ++k)
-                        umma_ts(t_dq, t_ds + k * 8, umma_desc_join(k_m + k * 128, hi), kIdescdQ, (j > 0 || k > 0) ? 1u : 0u);
-                    tc_commit(&bars->kv_empty[st]);
-                    if (!more) tc_commit(&bars->dq_done[t]);
-                    if (!Cfg::kSepdS && more) {  // S of the next step, over the dS that the product above reads
                         product(t_s, q_k, k_k0 + st_n * (Cfg::kStepBytes >> 4));
+                        product(t_dp, do_k, v_k0 + st_n * (Cfg::kStepBytes >> 4));
                         tc_commit(&bars->sp_full[0][t]);
                     }
-                }
-                __syncwarp();
-                if (more) {
+                    __syncwarp();
                     ++cq;
                     next_stage(&st_n, &ph_n);
                 }
-                next_stage(&st, &ph);
+                for (int j = j0; j < j1; ++j, ++c, ++done) {
+                    const bool more = j + 1 < j1;
+                    if (more) {  // dP (and S, where dS has columns of its own) of the next step, once this step's have been read
+                        ok = mbar_wait(&bars->kv_full[st_n], ph_n, abort_flag);
+                        if (ok) ok = mbar_wait(&bars->sp_free[0][t], (cq - 1) & 1, abort_flag);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (el) {
+                            if (Cfg::kSepdS) product(t_s, q_k, k_k0 + st_n * (Cfg::kStepBytes >> 4));
+                            product(t_dp, do_k, v_k0 + st_n * (Cfg::kStepBytes >> 4));
+                            if (Cfg::kSepdS) tc_commit(&bars->sp_full[0][t]);
+                        }
+                        __syncwarp();
+                    }
+                    ok = mbar_wait(&bars->ds_ready[c & 1][t], (c >> 1) & 1, abort_flag);
+                    // the previous item's dQ must have been read out of TMEM before it is overwritten
+                    if (ok && done == 0 && wt > 0) ok = mbar_wait(&bars->dq_free[t], (wt - 1) & 1, abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    // dQ += dS K_j: dS from TMEM (16 keys = 8 packed columns per instruction), K MN-major (rows = keys,
+                    // 64 head-dim elements per 128-byte row, the second 64-wide half kHalfStepBytes further).
+                    if (el) {
+                        const uint32_t t_ds = t_dq + Cfg::kColdS + (Cfg::kSepdS ? 32 * (c & 1) : 0);
+                        const uint32_t k_m = k_m0 + st * (Cfg::kStepBytes >> 4);
+#pragma unroll
+                        for (int k = 0; k < kStep / 16; ++k)
+                            umma_ts(t_dq, t_ds + k * 8, umma_desc_join(k_m + k * 128, hi), kIdescdQ, (done > 0 || k > 0) ? 1u : 0u);
+                        tc_commit(&bars->kv_empty[st]);
+                        if (j + 1 == n_t) tc_commit(&bars->dq_done[t]);
+                        if (!Cfg::kSepdS && more) {  // S of the next step, over the dS that the product above reads
+                            product(t_s, q_k, k_k0 + st_n * (Cfg::kStepBytes >> 4));
+                            tc_commit(&bars->sp_full[0][t]);
+                        }
+                    }
+                    __syncwarp();
+                    if (more) {
+                        ++cq;
+                        next_stage(&st_n, &ph_n);
+                    }
+                    next_stage(&st, &ph);
+                }
             }
         }
         if (!ok) break;
@@ -415,7 +445,9 @@ __device__ __forceinline__ void dq_rows(uint8_t* smem, DqBars* bars, uint32_t tm
         constexpr bool kInTurn = (D == 64);
         uint64_t next0 = 0, next1 = 0;
 
-        for (int j = 0; j < n_t; ++j, ++cnt) {
+        int skip, resume;
+        wk.left_out(blk, t, n_t, &skip, &resume);
+        for (int j = skip > 0 ? 0 : resume; j < n_t; j = j + 1 == skip ? resume : j + 1, ++cnt) {
             const int buf = kDelta ? (cnt & 1) : 0;
             ok = mbar_wait(&bars->sp_full[buf][t], (kDelta ? (cnt >> 1) : cnt) & 1, abort_flag);
             if (!ok) break;
@@ -706,9 +738,9 @@ cudaError_t configure_attn_dq() {
             if constexpr (D == 128) {
                 if (r == cudaSuccess) r = set(attn_dq_kernel<D, kTiles, kCausal, false, false>);
                 if (r == cudaSuccess) r = set(attn_dq_kernel<D, kTiles, kCausal, true, false>);
-                if constexpr (kTiles == 1 && kCausal) {
-                    if (r == cudaSuccess) r = set(attn_dq_kernel<D, 1, true, false, true>);
-                    if (r == cudaSuccess) r = set(attn_dq_kernel<D, 1, true, true, true>);
+                if constexpr (kCausal) {
+                    if (r == cudaSuccess) r = set(attn_dq_kernel<D, kTiles, true, false, true>);
+                    if (r == cudaSuccess) r = set(attn_dq_kernel<D, kTiles, true, true, true>);
                 }
             }
             return r;
@@ -740,14 +772,29 @@ cudaError_t launch_attn_dq(const CUtensorMap& tmQ, const CUtensorMap& tmK, const
 cudaError_t launch_window_dq(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
                              const CUtensorMap& tmdQ, bool strided, uint32_t orders, const float* LSE, const float* Delta,
                              const AttnShape& s, const Window& win, int num_sms, int* dev_status, cudaStream_t stream) {
-    const int n_blocks = (s.T + kBlockQ - 1) / kBlockQ, BH = s.B * s.H;
-    const int chunk = heads_per_chunk(BH, n_blocks, s.T, s.D, num_sms);
+    // Single tiles or pairs by the weights of plan_of; beyond a few rounds all items count as the last block's.  Pairs, single tiles:
+    // B=2, H=12 on 4, T=8192, window 1024, 4 sinks: 546, 564 us (the whole pass); backward alone, H=9 on 3, T=2304, window 700: 58.0,
+    // 48.8 us; H=32 on 8, T=2048, window 1024: 135.7, 133.5; H=8 on 2, T=1024, window 256: 40.2, 35.8.
+    const int n_tiles = (s.T + kBlockQ - 1) / kBlockQ, n_pairs = (n_tiles + 1) / 2, BH = s.B * s.H;
+    auto until_done = [&](int tiles, int n) -> long long {
+        auto steps = [&](long long i) {
+            return 2ll + key_span(win, (n - 1 - static_cast<int>(i / BH)) * tiles * kBlockQ, tiles * kBlockQ, s.T, kStep).n;
+        };
+        const long long items = static_cast<long long>(n) * BH;
+        return items <= 8ll * num_sms ? steps_until_done(items, num_sms, steps) : (items + num_sms - 1) / num_sms * steps(0);
+    };
+    const bool single = 5 * until_done(1, n_tiles) < 8 * until_done(2, n_pairs);
+    const int n_blocks = single ? n_tiles : n_pairs, chunk = heads_per_chunk(BH, n_blocks, s.T, s.D, num_sms);
     const dim3 grid(static_cast<unsigned>(n_blocks) * BH);
-    auto go = [&](auto kernel) {
-        return launch_overlapped(kernel, grid, dim3(kThreads), DqCfg<128, 1>::kSmemBytes, stream, tmQ, tmK, tmV, tmdO, tmdQ, LSE,
+    auto go = [&](auto kernel, int smem) {
+        return launch_overlapped(kernel, grid, dim3(kThreads), smem, stream, tmQ, tmK, tmV, tmdO, tmdQ, LSE,
                                  Delta, s.T, BH, s.H, orders, n_blocks, chunk, s.scale, dev_status, win);
     };
-    return strided ? go(attn_dq_kernel<128, 1, true, true, true>) : go(attn_dq_kernel<128, 1, true, false, true>);
+    if (single)
+        return strided ? go(attn_dq_kernel<128, 1, true, true, true>, DqCfg<128, 1>::kSmemBytes)
+                       : go(attn_dq_kernel<128, 1, true, false, true>, DqCfg<128, 1>::kSmemBytes);
+    return strided ? go(attn_dq_kernel<128, 2, true, true, true>, DqCfg<128, 2>::kSmemBytes)
+                   : go(attn_dq_kernel<128, 2, true, false, true>, DqCfg<128, 2>::kSmemBytes);
 }
 
 cudaError_t launch_attn_delta(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV,

@@ -6,6 +6,7 @@ them; K, V and their gradients may have fewer heads than Q, a divisor."""
 from __future__ import annotations
 
 import ctypes
+import operator
 
 from . import nova_attn as _na
 
@@ -24,6 +25,14 @@ def _lib():
     return lib
 
 
+def _ints(**named):
+    """Whole numbers that fit the C ABI's int, in order."""
+    for name, x in named.items():
+        if not -2**31 <= operator.index(x) < 2**31:
+            raise ValueError(f"{name} is out of range")
+    return [operator.index(x) for x in named.values()]
+
+
 def nova_window_fwd(Q, K, V, O, LSE, scale: float, window: int, sinks: int = 0, O_rest=None, stream=None) -> None:
     """O, LSE <- attention(Q, K, V); LSE is contiguous fp32 [B,H,T].  O_rest (strides of O): what rounding took from O, for
     nova_window_bwd_preprocess."""
@@ -40,7 +49,7 @@ def nova_window_bwd_preprocess(O, O_rest, dO, Delta, stream=None) -> None:
 
 
 def nova_window_bwd_workspace_bytes(B: int, H: int, H_kv: int, T: int, D: int, window: int, sinks: int = 0) -> int:
-    return int(_lib().nova_window_bwd_workspace_bytes(B, H, H_kv, T, D, window, sinks))
+    return int(_lib().nova_window_bwd_workspace_bytes(*_ints(B=B, H=H, H_kv=H_kv, T=T, D=D, window=window, sinks=sinks)))
 
 
 def nova_window_bwd(Q, K, V, dO, LSE, Delta, dQ, dK, dV, scale: float, window: int, sinks: int = 0, workspace=None,
@@ -53,7 +62,7 @@ def nova_window_bwd(Q, K, V, dO, LSE, Delta, dQ, dK, dV, scale: float, window: i
 
 
 def nova_window_decode_workspace_bytes(B: int, H: int, H_kv: int, T_max: int, D: int, window: int, sinks: int = 0) -> int:
-    return int(_lib().nova_window_decode_workspace_bytes(B, H, H_kv, T_max, D, window, sinks))
+    return int(_lib().nova_window_decode_workspace_bytes(*_ints(B=B, H=H, H_kv=H_kv, T_max=T_max, D=D, window=window, sinks=sinks)))
 
 
 def nova_window_decode(Q, K, V, lengths, O, LSE, scale: float, window: int, sinks: int = 0, workspace=None, stream=None) -> None:

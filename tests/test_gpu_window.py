@@ -125,6 +125,10 @@ SHAPES = [
     (1, 6, 2, 2600, 128, 300, 200),   # two tiles with sinks
     (2, 12, 1, 1100, 128, 1100, 0),   # long lists on few heads
     (1, 16, 1, 200, 64, 200, 0),
+    (6, 12, 4, 700, 128, 200, 70),    # pairs of query tiles in dQ
+    (12, 16, 16, 300, 128, 30, 1),    # the last pair has one tile
+    (5, 16, 2, 900, 128, 64, 130),
+    (4, 12, 4, 1500, 128, 300, 0),
 ]
 
 
@@ -257,6 +261,55 @@ def test_streams_and_graphs():
         p.check(100, 4)
 
 
+def test_strides_of_dimensions_of_size_one():
+    """A view may have any stride where there is one element: it is not used."""
+    na, nw = _libs()
+    g = torch.Generator().manual_seed(12)
+    T, D = 150, 64
+    q, k, v, do = (_randn(g, T, D).as_strided((1, 1, T, D), (3, 1, D, 1)) for _ in range(4))
+    o, rest, dq, dk, dv = (torch.empty((T, D), dtype=torch.bfloat16, device=DEV).as_strided((1, 1, T, D), (0, 5, D, 1)) for _ in range(5))
+    lse, delta = torch.empty((1, 1, T), device=DEV), torch.empty((1, 1, T), device=DEV)
+    nw.nova_window_fwd(q, k, v, o, lse, 0.125, 40, 3, O_rest=rest)
+    nw.nova_window_bwd_preprocess(o, rest, do, delta)
+    nw.nova_window_bwd(q, k, v, do, lse, delta, dq, dk, dv, 0.125, 40, 3)
+    na.nova_attn_poll_device_status()
+    ref_o, _, p = ref.forward(q.double(), k.double(), v.double(), 0.125, 40, 3)
+    assert ((o.double() - ref_o).abs() <= ref.forward_bound(p, v.double(), ref_o)).all()
+    grads, bounds, _ = ref.backward(q.double(), k.double(), v.double(), do.double(), 0.125, 40, 3)
+    for got, want, bound in zip((dq, dk, dv), grads, bounds):
+        assert ((got.double() - want).abs() <= bound).all()
+    one = q[:, :, -1:].as_strided((1, 1, 1, D), (1, 1, 1, 1), q.storage_offset() + (T - 1) * D)
+    o1, lse1 = torch.empty((1, 1, 1, D), dtype=torch.bfloat16, device=DEV), torch.empty((1, 1, 1), device=DEV)
+    nw.nova_window_decode(one, k, v, torch.tensor([T], dtype=torch.int32, device=DEV), o1, lse1, 0.125, 40, 3)
+    assert ((o1.double() - ref_o[:, :, -1:]).abs() <= ref.HALF * ref_o[:, :, -1:].abs() + 2.0**-14 * (p @ v.double().abs())[:, :, -1:]).all()
+
+
+def test_refusals():
+    na, nw = _libs()
+    p = Problem(1, 4, 2, 64, 64, False, seed=1, pad=0)
+    run = lambda **kw: nw.nova_window_fwd(*[kw.get(n, getattr(p, n)) for n in ("q", "k", "v", "o", "lse")], 0.125, kw.get("window", 8),
+                                          kw.get("sinks", 0), O_rest=kw.get("rest"))
+    for kw, error in (({"window": 2.5}, TypeError), ({"window": 2**31}, ValueError), ({"k": p.k[:, :, :32]}, ValueError),
+                      ({"v": p.q}, ValueError), ({"q": p.q.float()}, TypeError), ({"lse": p.lse[:, :2]}, TypeError),
+                      ({"q": p.q.transpose(2, 3)}, TypeError), ({"rest": p.rest.transpose(1, 2).contiguous().transpose(1, 2)}, ValueError),
+                      ({"o": p.o.cpu()}, TypeError)):
+        with pytest.raises(error):
+            run(**kw)
+    for kw, status in (({"window": 0}, na.ERR_SHAPE), ({"sinks": -1}, na.ERR_SHAPE), ({"k": p.k[:, :1].expand(1, 3, 64, 64), "v": p.v[:, :1].expand(1, 3, 64, 64)}, na.ERR_SHAPE),
+                       ({"k": p.k[:, :1].expand(1, 2, 64, 64)}, na.ERR_SHAPE)):
+        with pytest.raises(na.NovaAttnError) as e:
+            run(**kw)
+        assert e.value.status == status
+    small = torch.empty(8, dtype=torch.uint8, device=DEV)
+    with pytest.raises(na.NovaAttnError) as e:
+        nw.nova_window_bwd(p.q, p.k, p.v, p.do, p.lse, p.delta, p.dq, p.dk, p.dv, 0.125, 8, 0, workspace=small)
+    assert e.value.status == na.ERR_WORKSPACE
+    with pytest.raises(ValueError):  # one token per sequence
+        nw.nova_window_decode(p.q, p.k, p.v, torch.zeros(1, dtype=torch.int32, device=DEV), p.o, p.lse, 0.125, 8)
+    torch.cuda.synchronize()
+    assert (p.o == 7.0).all() and (p.dq == 7.0).all(), "a refused call must not launch anything"
+
+
 # ---------------------------------------------------------------- single tokens
 
 DECODE = [
@@ -303,7 +356,7 @@ def test_single_tokens(B, H, KV, T, D, window, sinks, lengths, by_token):
     assert ((lse.double() - want_lse)[~empty].abs() <= 3e-5 + 1e-6 * want_lse[~empty].abs()).all()
     assert (buf[:, 0] == 7.0).all() and (buf[:, -1] == 7.0).all()
     o2, lse2 = torch.empty_like(o), torch.empty_like(lse)
-    ws = torch.full((nw.nova_window_decode_workspace_bytes(B, H, KV, T, D, min(window, 2**31 - 1), sinks),), 255, dtype=torch.uint8, device=DEV)
+    ws = torch.full((nw.nova_window_decode_workspace_bytes(B, H, KV, T, D, window, sinks),), 255, dtype=torch.uint8, device=DEV)
     nw.nova_window_decode(q, k, v, length, o2, lse2, scale, window, sinks, workspace=ws if ws.numel() else None)
     assert torch.equal(o, o2) and torch.equal(lse, lse2), "the same bits in every run"
 

@@ -120,6 +120,10 @@ def test_workspace_queries(lib):
         assert nw.nova_window_bwd_workspace_bytes(*bad) == 0 and nw.nova_window_decode_workspace_bytes(*bad) == 0
     assert nw.nova_window_decode_workspace_bytes(1, 2, 1, 16, 64, 16, 0) == 0  # one run of keys: nothing to join
     assert nw.nova_window_decode_workspace_bytes(1, 2, 1, 10**6, 64, 10**6, 0) > 0
+    with pytest.raises(ValueError):
+        nw.nova_window_bwd_workspace_bytes(1, 2, 1, 64, 64, 2**31, 0)
+    with pytest.raises(TypeError):
+        nw.nova_window_decode_workspace_bytes(1, 2, 1, 64, 64, 8.5, 0)
 
 
 def test_rope_calls_refuse_bad_arguments(lib):
