@@ -48,7 +48,6 @@ __global__ void __launch_bounds__(kThreads) window_sum_kernel(const float* __res
 
 KvParts kv_parts(int BH, int T, const Window& win) {
     constexpr int kSms = 148;
-    constexpr int kLeast = 12;  // steps of a part: below that the ends of an item cost more than its steps
     KvParts p;
     p.n_tiles = (T + kBlockK - 1) / kBlockK;
     p.sink_tiles = std::min(p.n_tiles, (win.sinks + kBlockK - 1) / kBlockK);
@@ -62,18 +61,27 @@ KvParts kv_parts(int BH, int T, const Window& win) {
     };
     const long long cut_from = std::min<long long>(p.n_tiles, std::max<long long>(p.sink_tiles, n_q >= whole ? (n_q - whole) / per_tile + 1 : 0));
     const long long all = to_end(0, p.sink_tiles) + (cut_from - p.sink_tiles) * whole + to_end(cut_from, p.n_tiles);
-    const long long per_sm = all * win.group * BH / kSms;
+    const long long total = all * win.group * BH, per_sm = total / kSms, tiles = static_cast<long long>(p.n_tiles) * BH;
     auto cut = [&](int first, int last, long long most) -> int {  // parts of tiles whose longest list is the first, shortest the last
         const long long n = (list(first) + most - 1) / most;
         return static_cast<int>(std::max(1ll, std::min(n, list(last))));
     };
-    // A tile with sinks that is longer than an SM's share of all steps: into thirds of that (B=2, H=12 on 4, T=8192, D=128, window
-    // 1024, 4 sinks: a list of 384 steps, a share of 209: 404 us in one item, 256 so).  Shorter ones go first and hold nobody up
-    // (B=8, H=12, T=1024, D=64, window 256, 4 sinks, 16 steps of 30: 29.7 us, 39 in two parts).
-    if (p.sink_tiles > 0 && list(0) > per_sm) p.sink_parts = cut(0, p.sink_tiles - 1, std::max<long long>(kLeast, per_sm / 3));
+    // Small problems: dQ has SMs to spare, and its items and these run side by side as long as there is one SM for each.  Three
+    // quarters of what it leaves, because each part costs memory traffic, too (H=8 on 1, T=1024, window 256: at D=64 17.7 us with parts
+    // of 12 steps, 16.1 with 6; at D=128 with 4 sinks 35.7 with 12, 34.9 with 8, 33.8 with 4, and 39 where a tile with sinks is cut
+    // finer than that; T=512, window 128, D=64, H=2 on 1: 15.0 with 12, 13.1 with 4).
+    const long long spare = 3 * (kSms - win.group * tiles - tiles) / 4;
+    long long sink_least = 16, least = 12;  // below that the ends of an item cost more than its steps
+    if (spare > 0) least = std::min(least, std::max(4ll, (total + spare - 1) / spare));
+    if (least < 12) sink_least = least;
+    // A tile with sinks that is longer than an SM's share of all steps: into parts of that share (B=2, H=12 on 4, T=8192, D=128,
+    // window 1024, 4 sinks, a list of 384 steps, a share of 209: 571 us in one item, 388 in 2, 398 in 6; H=12 on 4, T=4096, D=128,
+    // window 300, 1 sink, 192 and 22: 231, 74 in 8, 88 in 12; H=8 on 8, T=16384, D=64, window 512, 256 and 82: 214, 103 in 4, 107 in 8).
+    // Shorter ones go first and hold nobody up (B=8, H=12, T=1024, D=64, window 256, 4 sinks, 16 steps of 30: 55 us, 63 in two parts).
+    if (p.sink_tiles > 0 && list(0) > per_sm) p.sink_parts = cut(0, p.sink_tiles - 1, std::max(sink_least, per_sm));
     // The others only where there are fewer of them than SMs.
     const long long rest = static_cast<long long>(p.n_tiles - p.sink_tiles) * BH;
-    if (rest > 0 && rest < kSms) p.parts = cut(p.sink_tiles, p.n_tiles - 1, std::max<long long>(kLeast, list(p.sink_tiles) * rest / kSms));
+    if (rest > 0 && rest < kSms) p.parts = cut(p.sink_tiles, p.n_tiles - 1, std::max(least, list(p.sink_tiles) * rest / kSms));
     return p;
 }
 
