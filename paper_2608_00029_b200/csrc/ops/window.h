@@ -39,7 +39,7 @@ struct DecodePlan {
     long long items;  // sequences x key/value heads x groups of 16 query heads
 };
 // Of the shape alone: the size of the workspace and the order of the sums follow from it.
-DecodePlan decode_plan(int B, int H, int H_kv, int T_max, int window, int sinks);
+DecodePlan decode_plan(int B, int H, int H_kv, int T_max, int D, int window, int sinks);
 cudaError_t launch_window_decode(const DecodeArgs& a, int D, long long items, int B, cudaStream_t stream);
 
 }  // namespace nova

@@ -146,7 +146,7 @@ int nova_window_bwd(const void* Q, const void* K, const void* V, const void* dO,
 
 size_t nova_window_decode_workspace_bytes(int B, int H, int H_kv, int T_max, int D, int window, int sinks) {
     if (check_window(B, H, H_kv, T_max, D, window, sinks) != NOVA_ATTN_OK) return 0;
-    return decode_bytes(decode_plan(B, H, H_kv, T_max, window, sinks), B, H, D);
+    return decode_bytes(decode_plan(B, H, H_kv, T_max, D, window, sinks), B, H, D);
 }
 
 int nova_window_decode(const void* Q, const void* K, const void* V, const int* lengths, void* O, float* LSE, int B, int H, int H_kv,
@@ -163,7 +163,7 @@ int nova_window_decode(const void* Q, const void* K, const void* V, const int* l
     if (int rc = check_strides(k_strides, D, &a.sk)) return rc;
     if (int rc = check_strides(v_strides, D, &a.sv)) return rc;
     if (int rc = check_strides(o_strides, D, &a.so)) return rc;
-    const DecodePlan p = decode_plan(B, H, H_kv, T_max, window, sinks);
+    const DecodePlan p = decode_plan(B, H, H_kv, T_max, D, window, sinks);
     if (p.items * p.splits > 0x7fffffffll) return NOVA_ATTN_ERR_SHAPE;
     const size_t need = decode_bytes(p, B, H, D);
     if (need > 0 && (!workspace || workspace_bytes < need)) return NOVA_ATTN_ERR_WORKSPACE;

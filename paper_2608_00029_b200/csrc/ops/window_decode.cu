@@ -25,6 +25,9 @@ namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps, kTile = 16;
 constexpr int kRows = 16;  // query heads of a CTA at most
+constexpr int kMaxCluster = 8;
+// CTAs of the kernel below that an SM holds, cols: groups of 8 query heads.
+__host__ __device__ constexpr int resident(int D, int cols) { return cols == 1 ? (D == 64 ? 5 : 3) : (D == 64 ? 3 : 2); }
 
 __device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                           uint32_t b1) {
@@ -69,7 +72,7 @@ __device__ __forceinline__ float2 load_peer2(uint32_t at) {
 
 // kCols: groups of 8 query heads.  kCluster: the runs of a row are a cluster (no CTA leaves before the others have read from it).
 template <int D, int kCols, bool kCluster>
-__global__ void __launch_bounds__(kThreads, kCols == 1 ? (D == 64 ? 5 : 3) : (D == 64 ? 3 : 2))
+__global__ void __launch_bounds__(kThreads, resident(D, kCols))
 window_decode_kernel(const __grid_constant__ DecodeArgs a) {
     __shared__ float s_o[kWarps][8 * kCols][D + 4];  // (rows of a warp's eight lanes in different banks)
     __shared__ float s_m[kWarps][8 * kCols], s_l[kWarps][8 * kCols];
@@ -235,10 +238,10 @@ window_decode_kernel(const __grid_constant__ DecodeArgs a) {
         cluster_sync();
         for (int x = split * kThreads + threadIdx.x; x < rows * (D / 4); x += a.splits * kThreads) {
             const int r = x / (D / 4), d = x % (D / 4) * 4;
-            float2 ml[8];
-            float4 v[8];
+            float2 ml[kMaxCluster];
+            float4 v[kMaxCluster];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < kMaxCluster; ++k) {
                 ml[k] = make_float2(-INFINITY, 0.f);
                 v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (k < a.splits) {
@@ -248,11 +251,11 @@ window_decode_kernel(const __grid_constant__ DecodeArgs a) {
             }
             float top = -INFINITY;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) top = fmaxf(top, ml[k].x);
+            for (int k = 0; k < kMaxCluster; ++k) top = fmaxf(top, ml[k].x);
             float sum_l = 0.f;
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < kMaxCluster; ++k) {
                 if (k >= a.splits) break;
                 const float f = ml[k].x == -INFINITY ? 0.f : ex2_approx(ml[k].x - top);
                 sum_l += f * ml[k].y;
@@ -336,19 +339,28 @@ __global__ void __launch_bounds__(kPer > 8 ? 32 * kPer : 256) window_join_kernel
 
 }  // namespace
 
-DecodePlan decode_plan(int B, int H, int H_kv, int T_max, int window, int sinks) {
+DecodePlan decode_plan(int B, int H, int H_kv, int T_max, int D, int window, int sinks) {
     DecodePlan p;
     const long long most = static_cast<long long>(window) + sinks;
-    const int n = static_cast<int>(most < T_max ? most : T_max), group = H / H_kv;
+    const long long n = most < T_max ? most : T_max;
+    const int group = H / H_kv;
     p.head_groups = (group + kRows - 1) / kRows;
-    const long long items = static_cast<long long>(B) * H_kv * p.head_groups;
-    // Runs of equal size: eight CTAs for each of the 148 SMs if the runs stay long enough for it, one tile a warp at least.
-    long long chunk = (n * items + 148 * 8 - 1) / (148 * 8);
+    p.items = static_cast<long long>(B) * H_kv * p.head_groups;
     constexpr int kLeast = kWarps * kTile;
-    chunk = (chunk + kLeast - 1) / kLeast * kLeast;
-    p.chunk = static_cast<int>(chunk < kLeast ? kLeast : chunk);
-    p.splits = (n + p.chunk - 1) / p.chunk;
-    p.items = items;
+    auto rounded = [](long long chunk) { return (chunk + kLeast - 1) / kLeast * kLeast; };
+    // Where it leaves no run longer than 1280 keys: as many CTAs as the GPU holds at once, so that all start together and the last is
+    // done when the first is (us against eight CTAs to an SM: B=16, H=32 on 8, D=128, 1024 keys: 14.8, 20.4; B=8, 4096 keys: 24.9, 31.2;
+    // B=1, 8192 keys: 11.9, 15.7; B=8, H=12, D=64, 1024 keys: 9.2, 11.2).  In clusters if they can be a few longer runs: B=4, H=32 on
+    // 8, D=128, 2048 keys: 11.4 with 8 to a row, 12.2 with 11 and a kernel to join them.
+    const long long at_once = 148ll * resident(D, group > 8 ? 2 : 1) / p.items;
+    long long splits = at_once > 1 ? at_once : 1;
+    if (splits > kMaxCluster && n <= kMaxCluster * 256) splits = kMaxCluster;
+    long long chunk = rounded((n + splits - 1) / splits);
+    // Longer: eight CTAs to an SM, which evens out sequences of different lengths.  (B=64, H=32 on 8, D=128, 2052 keys, the lengths
+    // random up to 4096: 67.4 us, 73.5 with four; H=64 on 4, D=64, B=32, random up to 8192: 42.5, with one run to an SM's CTA 54.2.)
+    if (chunk > 1280) chunk = rounded((n * p.items + 148 * 8 - 1) / (148 * 8));
+    p.chunk = static_cast<int>(chunk);
+    p.splits = static_cast<int>((n + chunk - 1) / chunk);
     return p;
 }
 
@@ -356,8 +368,8 @@ cudaError_t launch_window_decode(const DecodeArgs& a, int D, long long items, in
     const dim3 grid(static_cast<unsigned>(items * a.splits));
     auto go = [&](auto kernel) { return launch_overlapped(kernel, grid, dim3(kThreads), 0, stream, a); };
     const bool two = a.group > 8;
-    // A cluster holds its SMs until its longest run is through, which does not matter where there are SMs for all.
-    if (a.splits > 1 && a.splits <= 8 && items * a.splits <= 2 * 148) {
+    // A cluster holds its places until its longest run is through, which does not matter where there are places for all.
+    if (a.splits > 1 && a.splits <= kMaxCluster && items * a.splits <= 148 * resident(D, two ? 2 : 1)) {
         auto together = [&](auto kernel) {
             cudaLaunchConfig_t cfg = {};
             cfg.gridDim = grid;

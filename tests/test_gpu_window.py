@@ -325,6 +325,10 @@ DECODE = [
     (1, 3, 1, 5000, 128, 4000, 100, [5000]),
     (2, 2, 2, 3000, 64, 10**6, 0, [3000, 2999]),
     (3, 4, 2, 50, 64, 10, 3, [-5, 51, 10**9]),           # outside: the nearer end
+    (8, 12, 12, 1000, 64, 1000, 0, [1000, 999, 1, 0, 170, 500, 192, 193]),  # a cluster for each of many rows
+    (16, 16, 8, 500, 128, 450, 20, list(range(10, 490, 30))),
+    (3, 24, 2, 1700, 64, 1700, 0, [1700, 256, 900]),     # eight runs
+    (100, 4, 4, 1500, 64, 1400, 30, list(range(1, 1500, 15))),  # more rows than the GPU holds at once
 ]
 
 
