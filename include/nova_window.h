@@ -16,9 +16,10 @@
  * Conventions are those of nova_attn.h: device pointers, caller owns every buffer, work is only enqueued on `stream`, nothing is
  * allocated or synchronised, calls may be captured (after one call on the device), status codes are the NOVA_ATTN_* values and
  * nova_attn_poll_device_status applies.  bf16 tensors are addressed as (b, h, t, d) through strides as in the strided calls
- * there, with the same requirements; D is 64 or 128; scale is finite and > 0.  Elements of K, V, Q and dO that are not finite
- * make the results of other rows of their 128-row tile undefined, as there (in the single-token form they reach what keeps
- * them and nothing else).
+ * there, with the same requirements; D is 64 or 128; scale is finite and > 0.  An element of Q, K, V or dO that is not finite
+ * makes undefined, besides what it belongs in, the other results that come from its 128-row tile: those of every 128 queries (256 in
+ * the backward) or keys of which one meets one of that tile under the mask.  So tokens that pad a sequence have to be finite.  In
+ * the single-token form it reaches what keeps it and nothing else.
  *
  * Errors (checked on the host before any launch): NOVA_ATTN_ERR_NULL, NOVA_ATTN_ERR_SHAPE (sizes, strides, window < 1, sinks < 0,
  * H not a multiple of H_kv), NOVA_ATTN_ERR_UNSUPPORTED (D, or the device is not sm_100), NOVA_ATTN_ERR_ALIGNMENT,

@@ -8,7 +8,9 @@
 //   P^T  = exp2(S^T*c - LSE*log2e),  dS^T = P^T * (dP^T - Delta)   (bf16, over the S^T and dP^T they came from)
 //   dV  += P^T dO_s,  dK += dS^T Q_s                           (TMEM x smem, dO and Q read MN-major)
 // Items are handed out dynamically (WorkRing), heaviest first within a chunk of heads whose tensors stay in L2
-// together.  512 threads:
+// together.  With a window the heads are those of K and V, an item is a tile's list of steps in reach of all query heads that share its
+// head, or a part of it (KvParts): B=2, H=12 on 4, T=8192, window 1024, 4 sinks: 258 us under ncu, the tensor pipe 52 % busy.
+// 512 threads:
 //   warp 0      TMA producer: K_j double-buffered, V_j, and Q_s and dO_s through a ring of 64-query stages
 //   warp 1      UMMA issuer: S^T and dP^T run two steps ahead of dV and dK, across item boundaries
 //   warp 2      row loader: -LSE*log2e and -Delta of a step into shared memory

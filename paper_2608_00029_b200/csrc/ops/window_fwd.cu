@@ -5,15 +5,18 @@
 // them counts: TWO CTAs share an SM, each with half of its tensor memory, and what one of them waits for, at an item's ends or in
 // the chain products -> softmax -> product of a step, the other fills.  Within an item S runs a step ahead.
 // (The form with one CTA and two softmax groups, by which attn_fwd.cu works on single tiles, took 34.7 us for a window of 256 and 4
-// sinks at B=8, H=12, T=1024, D=64, longer than the whole triangle.)
+// sinks at B=8, H=12, T=1024, D=64, longer than the whole triangle; this one takes 24.5 with O_rest, 22.6 without.)
 //
 //   S = Q K_s^T      (smem x smem -> one of two buffers in TMEM)
 //   P = 2^(S c - m c) as bf16 over S, running maximum and sum in registers, one thread per row
 //   O += P V_s       (TMEM x smem); rescaled by the row's thread when its maximum has grown by more than 2^8
 //
-// What bounds it: 512 clocks of the exp2 unit per step (of 16 a clock), 320 (D=64) or 640 (D=128) of the tensor pipe.  Of a step's
-// 64 keys a warp leaves out the half that none of its 32 rows keeps, at the diagonal and at the window's far end; a step of
-// sinks takes products only as wide as there are sinks.
+// What bounds it: a step's chain, some 1400 clocks in a softmax warp besides its waits (512 of them the exp2 unit) and as long again
+// until the next S, against 512 clocks of the exp2 unit and 320 (D=64) or 640 (D=128) of the tensor pipe; 2900 clocks at an item's
+// end.  At D=64 the tensor pipe is 17 % busy and the exp2 unit 28 % (the shape above, cold), at D=128 47 and 44 % (B=2, H=12 on 4,
+// T=8192, window 1024: 110 us, 0.88 PFLOP/s of kept pairs; without any softmax 96).  Of a step's 64 keys a warp leaves out the half that
+// none of its 32 rows keeps, at the diagonal and at the window's far end; a step of sinks takes products only as wide as there
+// are sinks.
 // O (and what rounding takes from it) goes straight from the registers to memory, 64 bytes of a row per thread at a time:
 // there is no shared memory to stage it in, and no need to wait for it.
 //
