@@ -3,6 +3,7 @@ fallback: a missing library or a failed call raises.  Calls run on the device of
 from __future__ import annotations
 
 import ctypes
+import operator
 
 import torch
 
@@ -31,10 +32,12 @@ def nova_rope_frequencies(rotary: int, base: float = 10000.0, kind: str = "plain
     "bands" or "yarn" (`low` and `high` turns bound the last two's bands), as in the header."""
     if kind not in _KINDS:
         raise ValueError(f"kind must be one of {', '.join(_KINDS)}, not {kind!r}")
-    rotary = int(rotary)
+    rotary, original = operator.index(rotary), operator.index(original)
+    if not -2**31 <= rotary < 2**31 or not -2**63 <= original < 2**63:
+        raise ValueError("rotary or original is out of range")
     freq = (ctypes.c_float * max(1, rotary // 2))()
     amplitude = ctypes.c_float()
-    rc = _lib().nova_rope_frequencies(freq, ctypes.byref(amplitude), rotary, float(base), _KINDS[kind], float(factor), int(original),
+    rc = _lib().nova_rope_frequencies(freq, ctypes.byref(amplitude), rotary, float(base), _KINDS[kind], float(factor), original,
                                       float(low), float(high))
     if rc != _na.OK:
         raise _na.NovaAttnError(rc, "nova_rope_frequencies")

@@ -300,6 +300,11 @@ def test_frequencies(lib):
         assert e.value.status == na.ERR_SHAPE
     with pytest.raises(ValueError):
         nr.nova_rope_frequencies(64, kind="other")
+    for bad in ({"rotary": 2**32 + 2}, {"rotary": 64, "original": 2**63}):  # would wrap to numbers that it takes
+        with pytest.raises(ValueError):
+            nr.nova_rope_frequencies(**bad)
+    with pytest.raises(TypeError):
+        nr.nova_rope_frequencies(64.5)
 
 
 def test_reference_gradients_against_differences():
