@@ -1,6 +1,6 @@
 // One new token per sequence over a cache of keys and values, with a sliding window and sinks (include/nova_window.h).
 //
-// Memory bound: every kept key and value is read once, 4*D bytes, for the G query heads that share it (775 MB in 128 us, 6.05 TB/s, at
+// Memory bound: every kept key and value is read once, 4*D bytes, for the G query heads that share it (775 MB in 127 us, 6.1 TB/s, at
 // B=64, H=32 on 8, D=128, ragged lengths up to 8192, window 4096).  A CTA takes a run of
 // `chunk` kept keys of one key/value head of one sequence (so that sequences of all lengths make CTAs of one size), its four
 // warps every fourth 16 of them; what a CTA finds, its maximum, sum and weighted sum per query head, is joined with the
@@ -357,9 +357,11 @@ DecodePlan decode_plan(int B, int H, int H_kv, int T_max, int D, int window, int
     long long splits = at_once > 1 ? at_once : 1;
     if (splits > kMaxCluster && n <= kMaxCluster * 256) splits = kMaxCluster;
     long long chunk = rounded((n + splits - 1) / splits);
-    // Longer: eight CTAs to an SM, which evens out sequences of different lengths.  (B=64, H=32 on 8, D=128, 2052 keys, the lengths
-    // random up to 4096: 67.4 us, 73.5 with four; H=64 on 4, D=64, B=32, random up to 8192: 42.5, with one run to an SM's CTA 54.2.)
-    if (chunk > 1280) chunk = rounded((n * p.items + 148 * 8 - 1) / (148 * 8));
+    // Longer: twelve CTAs to an SM, which evens out sequences of different lengths.  (Time over that of the bytes, three draws of lengths
+    // each, with twelve and with eight: B=64, H=32 on 8, D=128, lengths up to 8192, of which 4100 keys are kept: 1.05, 1.08; B=16, all
+    // kept: 1.15, 1.23; H=64 on 4, D=64, B=32: 1.83, 2.00; B=2, up to 131072: 1.18, 1.20; B=4, up to 32768: 1.23, 1.14; all
+    // B=64 of full length 1.01, 1.04.)
+    if (chunk > 1280) chunk = rounded((n * p.items + 148 * 12 - 1) / (148 * 12));
     p.chunk = static_cast<int>(chunk);
     p.splits = static_cast<int>((n + chunk - 1) / chunk);
     return p;
