@@ -638,8 +638,9 @@ __device__ __forceinline__ void dq_body(const CUtensorMap* tmQ, const CUtensorMa
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = bars->tmem_base;
-    griddep_launch_dependents();
+    if (!kWindow) griddep_launch_dependents();
     griddep_wait();  // everything above overlaps the previous kernel of the stream
+    if (kWindow) griddep_launch_dependents();  // the dK/dV kernel, which needs nothing of dQ, but what was there before (ptx.cuh)
 
     if (warp == 0) {
         if (lane == 0) dq_producer<D, kTiles, kStrided, kWindow>(tmQ, tmK, tmV, tmdO, smem, bars, wk);

@@ -93,7 +93,7 @@ __host__ __device__ __forceinline__ void kv_part(int all, int part, int parts, i
     *n = static_cast<int>(static_cast<long long>(all) * (part + 1) / parts) - *first;
 }
 // BH: heads of K and V in all.  Of the shape alone.
-KvParts kv_parts(int BH, int T, int D, const Window& win);
+KvParts kv_parts(int BH, int T, const Window& win);
 cudaError_t launch_window_sum(const float* partial, const KvParts& parts, __nv_bfloat16* dK, __nv_bfloat16* dV, const TensorStrides& sdk,
                               const TensorStrides& sdv, int B, int H_kv, int T, int D, float scale, cudaStream_t stream);
 
@@ -204,7 +204,7 @@ cudaError_t launch_attn_dkdv(const CUtensorMap& tmQ, const CUtensorMap& tmK, con
                              const CUtensorMap& tmdO, const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided,
                              uint32_t orders, const float* LSE, const float* Delta, const AttnShape& s, int num_sms,
                              int* dev_status, cudaStream_t stream);
-// With the window: dK and dV have the heads of K and V, an item all query heads that share its key/value head.
+// With the window (ops/window_dkdv.cu): dK and dV have the heads of K and V, an item all query heads that share its key/value head.
 cudaError_t launch_window_dkdv(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
                                const CUtensorMap& tmdK, const CUtensorMap& tmdV, bool strided, uint32_t orders, const float* LSE,
                                const float* Delta, const AttnShape& s, const Window& win, const KvParts& parts, float* partial,
@@ -293,6 +293,8 @@ cudaError_t launch_lmhead_rows(const CUtensorMap& tmX, const CUtensorMap& tmW, c
 
 // The forward of the attention with a window (ops/window_fwd.cu).
 cudaError_t configure_window_fwd();
+// ops/window_dkdv.cu
+cudaError_t configure_window_dkdv();
 
 // Clears `bytes` (a multiple of 16) at the 16-byte aligned `ptr`.
 cudaError_t launch_zero(void* ptr, size_t bytes, int num_sms, cudaStream_t stream);

@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(kThreads) window_sum_kernel(const float* __res
 
 }  // namespace
 
-KvParts kv_parts(int BH, int T, int D, const Window& win) {
+KvParts kv_parts(int BH, int T, const Window& win) {
     constexpr int kSms = 148;
     KvParts p;
     p.n_tiles = (T + kBlockK - 1) / kBlockK;
@@ -67,12 +67,11 @@ KvParts kv_parts(int BH, int T, int D, const Window& win) {
         const long long n = (list(first) + most - 1) / most;
         return static_cast<int>(std::max(1ll, std::min(n, list(last))));
     };
-    // Small problems: parts until there is an SM for each, at D=64 one that dQ leaves, since the two kernels run side by side there.  Three
-    // quarters of them, because each part costs memory traffic, too (H=8 on 1, T=1024, window 256: at D=64 17.7 us with parts of 12
-    // steps, 16.1 with 6; at D=128 with 4 sinks 35.7 with 12, 34.9 with 8, 33.8 with 4, and 39 where a tile with sinks is cut finer
-    // than that; H=16 on 2, T=768, D=128, window 475, 1 sink: 47 with 12, 41.7 with 8; T=512, window 128, D=64, H=2 on 1: 15.0 with 12, 13.1
-    // with 4).
-    const long long spare = 3 * (kSms - tiles - (D == 64 ? win.group * tiles : 0)) / 4;
+    // Small problems: dQ has SMs to spare, and its items and these run side by side as long as there is one SM for each.  Three
+    // quarters of what it leaves, because each part costs memory traffic, too (backward, H=8 on 1, T=1024, window 256: at D=64 17.7 us
+    // with parts of 12 steps, 16.1 with 6; at D=128 with 4 sinks 24.6 with 8, 27 with 12, 47 with so many parts that they have to wait
+    // for dQ; T=512, window 128, D=64, H=2 on 1: 15.0 with 12, 13.1 with 4).
+    const long long spare = 3 * (kSms - win.group * tiles - tiles) / 4;
     long long sink_least = 16, least = 12;  // below that the ends of an item cost more than its steps
     if (spare > 0) least = std::min(least, std::max(4ll, (total + spare - 1) / spare));
     if (least < 12) sink_least = least;

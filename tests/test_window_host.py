@@ -261,11 +261,24 @@ def test_kernels_of_the_subfolder_wait_for_their_predecessor():
         for m in re.finditer(r"^(?:template[^\n]*\n)?__global__[^{;]*\{\n(.*?)^\}", text, re.M | re.S):
             body = m.group(1)
             kernels += 1
+            if "window_dkdv_kernel" in m.group(0):  # begins before dQ has ended, and ends after it
+                before, after = body.split("    kv_roles<")
+                assert "    if (threadIdx.x == 0 || warp == 2) griddep_taken_over();" in before and "griddep_wait();" in after
+                assert before.index("griddep_taken_over();") < before.index("kv_set_up(") < before.index("griddep_launch_dependents();")
+                continue
             assert body.count("griddep_launch_dependents();") == 1 and body.count("\n    griddep_wait();") == 1, name
             ahead = body.split("\n    griddep_wait();")[0]
             ahead = re.sub(r"auto \w+ = \[&\].*?\n    \};", "", ahead, flags=re.S)  # defined there, called later
             assert not re.search(r"\breturn\b|__ld|\[[^\]]*\] =|atomic|lengths|decode_keys", ahead), name
     assert kernels >= 3
+    # what dK/dV relies on: dQ lets it start when it has waited itself, and its row terms are read past L1
+    dq = open(os.path.join(CSRC, "attn_dq.cu")).read()
+    assert re.search(r"\n    griddep_wait\(\);[^\n]*\n    if \(kWindow\) griddep_launch_dependents\(\);", dq)
+    assert "    if (!kWindow) griddep_launch_dependents();" in dq and dq.count("griddep_launch_dependents();") == 2
+    roles = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "attn_dkdv.cuh")).read())
+    assert "return kWindow ? __ldcg(p) : *p;" in roles and not re.search(r"(LSE|Delta)\[", roles) and "griddep" not in roles
+    dkdv = open(os.path.join(CSRC, "attn_dkdv.cu")).read()
+    assert dkdv.index("\n    griddep_wait();") < dkdv.index("    kv_roles<")
 
 
 # ---------------------------------------------------------------- frequencies and the reference
