@@ -225,6 +225,37 @@ def test_same_bits_every_time():
             assert all(torch.equal(a, b) for a, b in zip(first, p.outputs()))
 
 
+@pytest.mark.parametrize("B,H,KV,T,D", [(1, 4, 2, 900, 64), (1, 4, 2, 900, 128), (4, 12, 4, 1100, 64), (4, 12, 4, 1100, 128)])
+def test_passes_one_behind_the_other(B, H, KV, T, D):
+    """Kernels begin before the one ahead of them has ended: nothing may be read that is still to be written, or written that is still to
+    be read.  Passes through the same buffers, by turns with other row terms and other parts."""
+    na, nw = _libs()
+    p = Problem(B, H, KV, T, D, False, seed=T + D)
+    masks = [(130, 4), (40, 0), (700, 130)]
+    ws = torch.empty(max(nw.nova_window_bwd_workspace_bytes(B, H, KV, T, D, w, s) for w, s in masks), dtype=torch.uint8, device=DEV)
+    alone = []
+    for w, s in masks:
+        p.run(w, s, workspace=ws)
+        torch.cuda.synchronize()
+        alone.append([x.clone() for x in p.outputs()])
+    got = []
+    for i in range(12):
+        p.run(*masks[i % 3], workspace=ws)
+        if i >= 9:
+            got.append([x.clone() for x in p.outputs()])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for i in range(9):
+            p.run(*masks[i % 3], workspace=ws)
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    na.nova_attn_poll_device_status()
+    for want, x in zip(alone, got):
+        assert all(torch.equal(a, b) for a, b in zip(want, x))
+    assert all(torch.equal(a, b) for a, b in zip(alone[2], p.outputs()))
+
+
 def test_streams_and_graphs():
     """Two problems on two streams at once, each captured into a graph and replayed on new inputs."""
     na, _ = _libs()
