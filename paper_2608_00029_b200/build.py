@@ -11,7 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libnova_attn.so")
 SOURCES = ["api.cu", "attn_fwd.cu", "attn_bwd.cu", "attn_bwd_pre.cu", "attn_dq.cu", "attn_dq64.cu", "attn_dkdv.cu", "attn_dkdv64.cu",
            "attn_bwd_static.cu", "lmhead.cu", "lmhead_rows.cu", "ops/rope.cu", "ops/window_api.cu",
-           "ops/window_decode.cu", "ops/window_dkdv.cu", "ops/window_fwd.cu", "ops/window_sum.cu"]
+           "ops/window_decode.cu", "ops/window_dkdv.cu", "ops/window_dq.cu",
+           "ops/window_fwd.cu", "ops/window_sum.cu"]
 BINDING = os.path.join(HERE, "_binding.so")
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared", "-cudart", "shared", "-Xlinker", "-soname=libnova_attn.so"]

@@ -79,6 +79,7 @@ int device_state(DeviceState** out) {
         if (e == cudaSuccess) e = configure_lmhead_rows();
         if (e == cudaSuccess) e = configure_window_fwd();
         if (e == cudaSuccess) e = configure_window_dkdv();
+        if (e == cudaSuccess) e = configure_window_dq();
         if (e == cudaSuccess) e = cudaGetSymbolAddress(reinterpret_cast<void**>(&st.dev_status), g_dev_status);
         if (e != cudaSuccess) { st.status = fail_cuda(e); return st.status; }
     }

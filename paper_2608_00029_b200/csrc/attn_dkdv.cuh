@@ -321,11 +321,6 @@ __device__ __forceinline__ void kv_mma(uint8_t* smem, KvBars* bars, uint32_t tme
     }
 }
 
-template <bool kWindow>
-__device__ __forceinline__ float kv_row_term(const float* __restrict__ p) {
-    return kWindow ? __ldcg(p) : *p;  // (past L1: with the window there was no griddep_wait)
-}
-
 // Row loader (one warp): -LSE*log2e and -Delta of each step, negated so that the compute warps fold them in with a packed
 // fma / add.  Queries past the end of the sequence get -inf, so that their P is exactly 0.  A NaN (or + inf) becomes 3e38:
 // P of that query is infinite where it is kept, as unusable as NaN, but 0 where the causal mask puts -inf in front of the
@@ -354,8 +349,8 @@ __device__ __forceinline__ void kv_row_loader(KvBars* bars, float* row_buf, cons
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     const int q = (s0 + sh) * kStep + lane + 32 * x;
-                    l[u][x] = (q < wk.T) ? kv_row_term<kWindow>(LSE + base + q) : INFINITY;
-                    d[u][x] = (q < wk.T) ? kv_row_term<kWindow>(Delta + base + q) : 0.f;
+                    l[u][x] = (q < wk.T) ? LSE[base + q] : INFINITY;
+                    d[u][x] = (q < wk.T) ? Delta[base + q] : 0.f;
                 }
                 ++sh;
                 if (kWindow && sh == per) {  // (what is loaded past the item's last step is not used)

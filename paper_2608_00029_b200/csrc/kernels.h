@@ -293,8 +293,9 @@ cudaError_t launch_lmhead_rows(const CUtensorMap& tmX, const CUtensorMap& tmW, c
 
 // The forward of the attention with a window (ops/window_fwd.cu).
 cudaError_t configure_window_fwd();
-// ops/window_dkdv.cu
+// ops/window_dkdv.cu, ops/window_dq.cu
 cudaError_t configure_window_dkdv();
+cudaError_t configure_window_dq();
 
 // Clears `bytes` (a multiple of 16) at the 16-byte aligned `ptr`.
 cudaError_t launch_zero(void* ptr, size_t bytes, int num_sms, cudaStream_t stream);

@@ -134,10 +134,10 @@ int nova_window_bwd(const void* Q, const void* K, const void* V, const void* dO,
             e = launch_window_dkdv64(tmQs, tmK, tmV, tmdOs, tmdK, tmdV, strided, orders_kv, LSE, Delta, s, win, parts, partial,
                                      st->dev_status, cs);
     } else {
-        e = launch_window_dq(tmQ, tmKs, tmVs, tmdO, tmdQ, strided, orders_dq, LSE, Delta, s, win, st->num_sms, st->dev_status, cs);
+        e = launch_window_dkdv(tmQs, tmK, tmV, tmdOs, tmdK, tmdV, strided, orders_kv, LSE, Delta, s, win, parts, partial, st->dev_status,
+                               cs);
         if (e == cudaSuccess)
-            e = launch_window_dkdv(tmQs, tmK, tmV, tmdOs, tmdK, tmdV, strided, orders_kv, LSE, Delta, s, win, parts, partial,
-                                   st->dev_status, cs);
+            e = launch_window_dq(tmQ, tmKs, tmVs, tmdO, tmdQ, strided, orders_dq, LSE, Delta, s, win, st->num_sms, st->dev_status, cs);
     }
     if (e == cudaSuccess && parts.slots(1) > 0)
         e = launch_window_sum(partial, parts, static_cast<__nv_bfloat16*>(dK), static_cast<__nv_bfloat16*>(dV), sdk, sdv, B, H_kv, T, D, scale, cs);

@@ -1,10 +1,8 @@
 // dK and dV of the attention with a window at D = 128: the roles of attn_dkdv.cu.  The heads are those of K and V; an item is a tile's
 // list of steps in reach of all query heads that share its head, or a part of it (KvParts).  B=2, H=12 on 4, T=8192, window 1024, 4
 // sinks: 258 us under ncu, the tensor pipe 52 % busy.
-//
-// Started while dQ runs, of which it needs nothing (ptx.cuh): where the kernel waited for dQ first, the backward of H=4 on 2, T=993,
-// window 93, 150 sinks took 28.2 us, now 18.5; of H=8 on 1, T=1024, window 256, 4 sinks 33.9, now 24.6; the training pass of the shape
-// above 540, now 530.
+// dQ (window_dq.cu) starts while this kernel runs: where the one waited for the other, the backward of H=4 on 2, T=993, window 93, 150
+// sinks took 28.2 us, now 17.9; of H=8 on 1, T=1024, window 256, 4 sinks 33.9, now 24.2; the training pass of the shape above 540, now 517.
 #include "../attn_dkdv.cuh"
 
 namespace nova {
@@ -30,15 +28,14 @@ window_dkdv_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const KvWork<true> wk{BH, parts.n_tiles, BH, T, H, orders, true, win, parts};
 
-    if (threadIdx.x == 0 || warp == 2) griddep_taken_over();  // the threads that will read global memory
     const uint32_t tmem_base = kv_set_up(bars, tmQ, tmK, tmV, tmdO, tmdK, tmdV, warp);
-    griddep_launch_dependents();
+    griddep_wait();  // everything above overlaps the previous kernel of the stream
+    griddep_launch_dependents();  // the dQ kernel, which needs nothing of dK and dV, but what was there before (ptx.cuh)
     kv_roles<true, kStrided, true>(smem, bars, tmem_base, tmQ, tmK, tmV, tmdO, tmdK, tmdV, partial, LSE, Delta, scale, wk, warp, lane);
 
     tc_fence_before();
     __syncthreads();
     if (warp == 1) tmem_dealloc(tmem_base, kTmemCols);
-    griddep_wait();  // what waits for this kernel waits for dQ too
     if (threadIdx.x == 0 && bars->abort_flag != 0) atomicExch(dev_status, kDevTimeout);
 }
 

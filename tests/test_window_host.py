@@ -261,24 +261,29 @@ def test_kernels_of_the_subfolder_wait_for_their_predecessor():
         for m in re.finditer(r"^(?:template[^\n]*\n)?__global__[^{;]*\{\n(.*?)^\}", text, re.M | re.S):
             body = m.group(1)
             kernels += 1
-            if "window_dkdv_kernel" in m.group(0):  # begins before dQ has ended, and ends after it
-                before, after = body.split("    kv_roles<")
-                assert "    if (threadIdx.x == 0 || warp == 2) griddep_taken_over();" in before and "griddep_wait();" in after
-                assert before.index("griddep_taken_over();") < before.index("kv_set_up(") < before.index("griddep_launch_dependents();")
+            if "window_dq_kernel" in m.group(0):  # begins before dK/dV has ended, and ends after it
+                before, after = body.split("    dq_roles<")
+                assert "    if (threadIdx.x == 0 || warp >= 4) griddep_taken_over();" in before and "\n    griddep_wait();" in after
+                assert before.index("griddep_taken_over();") < before.index("dq_set_up<") < before.index("griddep_launch_dependents();")
+                continue
+            if "window_dkdv_kernel" in m.group(0):  # lets it, having waited itself (and waits before it gives up)
+                assert re.search(r"\n    griddep_wait\(\);\s+griddep_launch_dependents\(\);\s+kv_roles<", body)
+                assert re.search(r"griddep_wait\(\);\s+if \(threadIdx.x == 0\) atomicExch\([^;]*;\s+return;", body) and body.count("return") == 1
                 continue
             assert body.count("griddep_launch_dependents();") == 1 and body.count("\n    griddep_wait();") == 1, name
             ahead = body.split("\n    griddep_wait();")[0]
             ahead = re.sub(r"auto \w+ = \[&\].*?\n    \};", "", ahead, flags=re.S)  # defined there, called later
             assert not re.search(r"\breturn\b|__ld|\[[^\]]*\] =|atomic|lengths|decode_keys", ahead), name
     assert kernels >= 3
-    # what dK/dV relies on: dQ lets it start when it has waited itself, and its row terms are read past L1
-    dq = open(os.path.join(CSRC, "attn_dq.cu")).read()
-    assert re.search(r"\n    griddep_wait\(\);[^\n]*\n    if \(kWindow\) griddep_launch_dependents\(\);", dq)
-    assert "    if (!kWindow) griddep_launch_dependents();" in dq and dq.count("griddep_launch_dependents();") == 2
-    roles = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, "attn_dkdv.cuh")).read())
-    assert "return kWindow ? __ldcg(p) : *p;" in roles and not re.search(r"(LSE|Delta)\[", roles) and "griddep" not in roles
-    dkdv = open(os.path.join(CSRC, "attn_dkdv.cu")).read()
-    assert dkdv.index("\n    griddep_wait();") < dkdv.index("    kv_roles<")
+    # past L1, because dQ did not wait; and the roles that both kernels share wait for nothing but barriers
+    roles = {n: re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, n)).read()) for n in ("attn_dq.cuh", "attn_dkdv.cuh")}
+    assert "return kWindow ? __ldcg(p) : *p;" in roles["attn_dq.cuh"] and not re.search(r"(LSE|Delta)\[", roles["attn_dq.cuh"])
+    assert not any("griddep" in r for r in roles.values())
+    for n, call in (("attn_dq.cu", "    dq_roles<"), ("attn_dkdv.cu", "    kv_roles<")):
+        text = open(os.path.join(CSRC, n)).read()
+        assert text.index("\n    griddep_wait();") < text.index(call) and text.count(call) == 1, n
+    api = open(os.path.join(CSRC, "ops", "window_api.cu")).read()
+    assert re.search(r"launch_window_dkdv\([^;]*;\s+if \(e == cudaSuccess\)\s+e = launch_window_dq\(", api)
 
 
 # ---------------------------------------------------------------- frequencies and the reference
