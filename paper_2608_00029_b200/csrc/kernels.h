@@ -93,7 +93,7 @@ __host__ __device__ __forceinline__ void kv_part(int all, int part, int parts, i
     *n = static_cast<int>(static_cast<long long>(all) * (part + 1) / parts) - *first;
 }
 // BH: heads of K and V in all.  Of the shape alone.
-KvParts kv_parts(int BH, int T, const Window& win);
+KvParts kv_parts(int BH, int T, int D, const Window& win);
 cudaError_t launch_window_sum(const float* partial, const KvParts& parts, __nv_bfloat16* dK, __nv_bfloat16* dV, const TensorStrides& sdk,
                               const TensorStrides& sdv, int B, int H_kv, int T, int D, float scale, cudaStream_t stream);
 

@@ -81,7 +81,7 @@ int nova_window_bwd_preprocess(const void* O, const void* O_rest, const void* dO
 
 size_t nova_window_bwd_workspace_bytes(int B, int H, int H_kv, int T, int D, int window, int sinks) {
     if (check_window(B, H, H_kv, T, D, window, sinks) != NOVA_ATTN_OK) return 0;
-    return bwd_bytes(B, H_kv, D, kv_parts(B * H_kv, T, window_of(H, H_kv, T, window, sinks)));
+    return bwd_bytes(B, H_kv, D, kv_parts(B * H_kv, T, D, window_of(H, H_kv, T, window, sinks)));
 }
 
 int nova_window_bwd(const void* Q, const void* K, const void* V, const void* dO, const float* LSE, const float* Delta, void* dQ, void* dK,
@@ -100,7 +100,7 @@ int nova_window_bwd(const void* Q, const void* K, const void* V, const void* dO,
     if (int rc = check_strides(dk_strides, D, &sdk)) return rc;
     if (int rc = check_strides(dv_strides, D, &sdv)) return rc;
     const Window win = window_of(H, H_kv, T, window, sinks);
-    const KvParts parts = kv_parts(B * H_kv, T, win);
+    const KvParts parts = kv_parts(B * H_kv, T, D, win);
     if (!workspace || workspace_bytes < bwd_bytes(B, H_kv, D, parts)) return NOVA_ATTN_ERR_WORKSPACE;
     if (parts.items(static_cast<long long>(B) * H_kv) > 0x7fffffffll) return NOVA_ATTN_ERR_SHAPE;
     if (!aligned16(workspace)) return NOVA_ATTN_ERR_ALIGNMENT;

@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(kThreads) window_sum_kernel(const float* __res
 
 }  // namespace
 
-KvParts kv_parts(int BH, int T, const Window& win) {
+KvParts kv_parts(int BH, int T, int D, const Window& win) {
     constexpr int kSms = 148;
     KvParts p;
     p.n_tiles = (T + kBlockK - 1) / kBlockK;
@@ -67,21 +67,29 @@ KvParts kv_parts(int BH, int T, const Window& win) {
         const long long n = (list(first) + most - 1) / most;
         return static_cast<int>(std::max(1ll, std::min(n, list(last))));
     };
-    // Small problems: dQ has SMs to spare, and its items and these run side by side as long as there is one SM for each.  Three
-    // quarters of what it leaves, because each part costs memory traffic, too (backward, H=8 on 1, T=1024, window 256: at D=64 17.7 us
-    // with parts of 12 steps, 16.1 with 6; at D=128 with 4 sinks 24.6 with 8, 27 with 12, 47 with so many parts that they have to wait
-    // for dQ; T=512, window 128, D=64, H=2 on 1: 15.0 with 12, 13.1 with 4).
+    // Small problems: the items of dQ and these run side by side as long as there is an SM for each.  Three quarters of what dQ leaves,
+    // because each part costs memory traffic, too (backward, H=8 on 1, T=1024, window 256: at D=64 17.7 us with parts of 12 steps, 16.1
+    // with 6; at D=128 with 4 sinks 25 with 8, 26 with 12; T=512, window 128, D=64, H=2 on 1: 15.0 with 12, 13.1 with 4).
     const long long spare = 3 * (kSms - win.group * tiles - tiles) / 4;
-    long long sink_least = 16, least = 12;  // below that the ends of an item cost more than its steps
-    if (spare > 0) least = std::min(least, std::max(4ll, (total + spare - 1) / spare));
-    if (least < 12) sink_least = least;
-    // A tile with sinks that is longer than an SM's share of all steps: into parts of that share (B=2, H=12 on 4, T=8192, D=128,
-    // window 1024, 4 sinks, a list of 384 steps, a share of 209: 571 us in one item, 388 in 2, 398 in 6; H=12 on 4, T=4096, D=128,
-    // window 300, 1 sink, 192 and 22: 231, 74 in 8, 88 in 12; H=8 on 8, T=16384, D=64, window 512, 256 and 82: 214, 103 in 4, 107 in 8).
-    // Shorter ones go first and hold nobody up (B=8, H=12, T=1024, D=64, window 256, 4 sinks, 16 steps of 30: 55 us, 63 in two parts).
-    if (p.sink_tiles > 0 && list(0) > per_sm) p.sink_parts = cut(0, p.sink_tiles - 1, std::max(sink_least, per_sm));
-    // The others only where there are fewer of them than SMs.
+    const long long few = spare > 0 ? std::max(4ll, (total + spare - 1) / spare) : total;
     const long long rest = static_cast<long long>(p.n_tiles - p.sink_tiles) * BH;
+    if (D == 128) {
+        // dQ comes behind and fills up what these leave: no part longer than an SM's share of the steps of both (a step of dQ takes two
+        // thirds of one here).  B=2, H=12 on 4, T=8192, window 1024, 4 sinks, a list of 384 steps, a share of 349: 419 us in one item,
+        // 370 in 2; H=12 on 4, T=4096, window 300, 1 sink, 192 and 38: 220, 61 in 6, 66 in 16; H=16 on 4, T=4096, window 512, all lists of
+        // 40, 55: 80, 93 in 2; H=16 on 2, T=768, window 475, 1 sink, 96 and 80, 8: 104, 31 in 12 and 8, 35 in 6 and 6.  Parts without
+        // sinks, which come later and are more, may be a third longer: H=16 on 4, T=1024, window 1024, 64 steps, 12: 34 in 4, 40 in 5.
+        const long long most = std::max(std::min(few, 8ll), 5 * total / (3 * kSms));
+        if (p.sink_tiles > 0) p.sink_parts = cut(0, p.sink_tiles - 1, most);
+        if (rest > 0) p.parts = cut(p.sink_tiles, p.n_tiles - 1, most * 4 / 3);
+        return p;
+    }
+    // dQ goes ahead, and the last of these to end should not be a long one.  A tile with sinks that is longer than an SM's share of all
+    // steps: into parts of that share (H=8 on 8, T=16384, window 512, 4 sinks, a list of 256 steps, a share of 82: 214 us in one item, 103
+    // in 4, 107 in 8).  Shorter ones go first and hold nobody up (B=8, H=12, T=1024, window 256, 4 sinks, 16 steps of 30: 55 us, 63
+    // in two parts).  The others only where there are fewer of them than SMs.
+    const long long least = std::min(few, 12ll), sink_least = few < 12 ? few : 16;  // below that the ends of an item cost more than its steps
+    if (p.sink_tiles > 0 && list(0) > per_sm) p.sink_parts = cut(0, p.sink_tiles - 1, std::max(sink_least, per_sm));
     if (rest > 0 && rest < kSms) p.parts = cut(p.sink_tiles, p.n_tiles - 1, std::max(least, list(p.sink_tiles) * rest / kSms));
     return p;
 }
