@@ -51,9 +51,10 @@ cudaError_t configure_window_dq() {
 cudaError_t launch_window_dq(const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const CUtensorMap& tmdO,
                              const CUtensorMap& tmdQ, bool strided, uint32_t orders, const float* LSE, const float* Delta,
                              const AttnShape& s, const Window& win, int num_sms, int* dev_status, cudaStream_t stream) {
-    // Single tiles or pairs by the weights of attn_dq.cu; beyond a few rounds all items count as the last block's.  Pairs, single tiles:
-    // B=2, H=12 on 4, T=8192, window 1024, 4 sinks: 546, 564 us (the whole pass); backward alone, H=9 on 3, T=2304, window 700: 58.0,
-    // 48.8 us; H=32 on 8, T=2048, window 1024: 135.7, 133.5; H=8 on 2, T=1024, window 256: 40.2, 35.8.
+    // Single tiles or pairs by the weights of attn_dq.cu; beyond a few rounds all items count as the last block's.  Backward, pairs and
+    // single tiles: B=2, H=12 on 4, T=8192, window 1024, 4 sinks: 369, 383 us; B=4, H=32 on 8, T=2048, window 512: 281, 287; H=8 on 2,
+    // T=2048, window 512: 44.1, 38.8; H=9 on 3, T=2304, window 700: 47.4, 43.2; H=16 on 4, T=4096, window 512, where the rule is wrong:
+    // 80.0, 77.1.
     const int n_tiles = (s.T + kBlockQ - 1) / kBlockQ, n_pairs = (n_tiles + 1) / 2, BH = s.B * s.H;
     auto until_done = [&](int tiles, int n) -> long long {
         auto steps = [&](long long i) {
