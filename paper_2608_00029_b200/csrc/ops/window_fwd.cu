@@ -8,7 +8,8 @@
 // sinks at B=8, H=12, T=1024, D=64, longer than the whole triangle; this one takes 24.5 with O_rest, 22.6 without.)
 //
 //   S = Q K_s^T      (smem x smem -> one of two buffers in TMEM)
-//   P = 2^(S c - m c) as bf16 over S, running maximum and sum in registers, one thread per row
+//   P = 2^(S c - m c) as bf16 over S (and what rounding takes from it beside it: launch_window_fwd), running maximum and sum in
+//       registers, one thread per row
 //   O += P V_s       (TMEM x smem); rescaled by the row's thread when its maximum has grown by more than 2^8
 //
 // What bounds it: a step's chain, some 1400 clocks in a softmax warp besides its waits (512 of them the exp2 unit) and as long again
@@ -21,6 +22,8 @@
 // there is no shared memory to stage it in, and no need to wait for it.
 //
 // 192 threads: warp 0 TMA producer, warp 1 UMMA issuer, warps 2-5 softmax.  Items are handed out dynamically (WorkRing).
+#include <type_traits>
+
 #include "../api.h"
 #include "../ptx.cuh"
 #include "window.h"
@@ -32,6 +35,7 @@ constexpr int kThreads = 192;
 constexpr int kTmemCols = 256;
 constexpr int kStep = kKeyStep;
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
+constexpr int kFewKeys = 64;  // (see launch_window_fwd)
 
 template <int D>
 struct Cfg {
@@ -149,7 +153,7 @@ __device__ __forceinline__ void producer(const CUtensorMap* tmQ, const CUtensorM
 }
 
 // UMMA issuer: the whole warp in uniform control flow, one elected lane issues.
-template <int D>
+template <int D, bool kSplit>
 __device__ __forceinline__ void mma(uint8_t* smem, Bars* bars, uint32_t tmem_base, const Work& wk) {
     using C = Cfg<D>;
     volatile int* abort_flag = &bars->abort_flag;
@@ -234,9 +238,12 @@ __device__ __forceinline__ void mma(uint8_t* smem, Bars* bars, uint32_t tmem_bas
                 const int chunks = (wk.width(span, j) + 15) / 16;
                 const uint32_t p = tmem_base + C::kColS + kStep * (g & 1), v = v_m0 + st_v * (C::kStepBytes >> 4);
 #pragma unroll
-                for (int k = 0; k < kStep / 16; ++k)
-                    if (k < chunks)
+                for (int k = 0; k < kStep / 16; ++k) {
+                    if (k < chunks) {
                         umma_ts(tmem_base + C::kColO, p + k * 8, umma_desc_join(v + k * 128, hi), kIdescPV, (j > 0 || k > 0) ? 1u : 0u);
+                        if (kSplit) umma_ts(tmem_base + C::kColO, p + 32 + k * 8, umma_desc_join(v + k * 128, hi), kIdescPV, 1u);
+                    }
+                }
                 tc_commit(&bars->pv_done);
                 tc_commit(&bars->v_empty[st_v]);
                 if (j + 1 == n) tc_commit(&bars->o_done);
@@ -259,6 +266,11 @@ __device__ __forceinline__ void mma(uint8_t* smem, Bars* bars, uint32_t tmem_bas
     }
 }
 
+// What rounding took from two numbers, rounded in its turn.
+__device__ __forceinline__ uint32_t rest_of(uint32_t packed, float x, float y) {
+    return pack_bf16x2(x - __uint_as_float(packed << 16), y - __uint_as_float(packed & 0xffff0000u));
+}
+
 // 32 bytes: one access where the row is aligned to them.
 __device__ __forceinline__ void store_32(uint16_t* p, const uint32_t* v, bool aligned) {
     if (aligned) {
@@ -271,7 +283,7 @@ __device__ __forceinline__ void store_32(uint16_t* p, const uint32_t* v, bool al
     }
 }
 
-template <int D>
+template <int D, bool kSplit>
 __device__ __forceinline__ void softmax(Bars* bars, uint32_t tmem_base, uint16_t* __restrict__ O, uint16_t* __restrict__ rest,
                                         float* __restrict__ LSE, const TensorStrides& so, bool aligned, float scale, const Work& wk,
                                         int swarp, int lane) {
@@ -360,7 +372,7 @@ __device__ __forceinline__ void softmax(Bars* bars, uint32_t tmem_base, uint16_t
             uint64_t acc[4] = {0, 0, 0, 0};
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                uint32_t pk[16];
+                uint32_t pk[16], lo[kSplit ? 16 : 1];
                 if (need[h]) {
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
@@ -373,12 +385,17 @@ __device__ __forceinline__ void softmax(Bars* bars, uint32_t tmem_base, uint16_t
                         acc[i / 2 % 4 + 1] = f32x2_add(acc[i / 2 % 4 + 1], f32x2_pack(p2, p3));
                         pk[i / 2] = pack_bf16x2(p0, p1);
                         pk[i / 2 + 1] = pack_bf16x2(p2, p3);
+                        if constexpr (kSplit) {
+                            lo[i / 2] = rest_of(pk[i / 2], p0, p1);
+                            lo[i / 2 + 1] = rest_of(pk[i / 2 + 1], p2, p3);
+                        }
                     }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) pk[i] = 0u;
+                    for (int i = 0; i < 16; ++i) pk[i] = lo[kSplit ? i : 0] = 0u;
                 }
                 tmem_st_x16(t_s + 16 * h, pk);
+                if constexpr (kSplit) tmem_st_x16(t_s + 32 + 16 * h, lo);
             }
             float a0, a1, a2, a3;
             f32x2_unpack(f32x2_add(acc[0], acc[2]), a0, a1);
@@ -409,7 +426,7 @@ __device__ __forceinline__ void softmax(Bars* bars, uint32_t tmem_base, uint16_t
             for (int x = 0; x < 16; ++x) {
                 const float o0 = __uint_as_float(a[2 * x]) * inv_l, o1 = __uint_as_float(a[2 * x + 1]) * inv_l;
                 v[x] = pack_bf16x2(o0, o1);
-                r[x] = pack_bf16x2(o0 - __uint_as_float(v[x] << 16), o1 - __uint_as_float(v[x] & 0xffff0000u));
+                r[x] = rest_of(v[x], o0, o1);
             }
             if (row < T) {
                 store_32(O + at + cb, v, aligned);
@@ -425,7 +442,7 @@ __device__ __forceinline__ void softmax(Bars* bars, uint32_t tmem_base, uint16_t
     }
 }
 
-template <int D, bool kStrided>
+template <int D, bool kStrided, bool kSplit>
 __global__ void __launch_bounds__(kThreads, 2)
 window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                   uint16_t* __restrict__ O, uint16_t* __restrict__ rest, float* __restrict__ LSE, const TensorStrides so,
@@ -472,9 +489,9 @@ window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     if (warp == 0) {
         if (lane == 0) producer<D, kStrided>(&tmQ, &tmK, &tmV, smem, bars, wk);
     } else if (warp == 1) {
-        mma<D>(smem, bars, tmem_base, wk);
+        mma<D, kSplit>(smem, bars, tmem_base, wk);
     } else {
-        softmax<D>(bars, tmem_base, O, rest, LSE, so, aligned, scale, wk, warp & 3, lane);
+        softmax<D, kSplit>(bars, tmem_base, O, rest, LSE, so, aligned, scale, wk, warp & 3, lane);
     }
 
     tc_fence_before();
@@ -483,16 +500,26 @@ window_fwd_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
     if (threadIdx.x == 0 && bars->abort_flag != 0) atomicExch(dev_status, kDevTimeout);
 }
 
+// Calls f with the kernel that is meant and its shared memory.
+template <typename F>
+cudaError_t with_kernel(int D, bool strided, bool split, F&& f) {
+    auto of = [&](auto d, auto st) {
+        constexpr int kD = decltype(d)::value;
+        constexpr bool kStrided = decltype(st)::value;
+        return split ? f(window_fwd_kernel<kD, kStrided, true>, Cfg<kD>::kSmemBytes) : f(window_fwd_kernel<kD, kStrided, false>, Cfg<kD>::kSmemBytes);
+    };
+    auto with_d = [&](auto d) { return strided ? of(d, std::true_type{}) : of(d, std::false_type{}); };
+    return D == 64 ? with_d(std::integral_constant<int, 64>{}) : with_d(std::integral_constant<int, 128>{});
+}
+
 }  // namespace
 
 cudaError_t configure_window_fwd() {
-    cudaError_t e = cudaFuncSetAttribute(window_fwd_kernel<64, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<64>::kSmemBytes);
-    if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(window_fwd_kernel<64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<64>::kSmemBytes);
-    if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(window_fwd_kernel<128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<128>::kSmemBytes);
-    if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(window_fwd_kernel<128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<128>::kSmemBytes);
+    cudaError_t e = cudaSuccess;
+    for (int k = 0; k < 8 && e == cudaSuccess; ++k)
+        e = with_kernel(k & 1 ? 64 : 128, (k & 2) != 0, (k & 4) != 0, [](auto kernel, int smem) {
+            return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        });
     return e;
 }
 
@@ -503,13 +530,15 @@ cudaError_t launch_window_fwd(const CUtensorMap& tmQ, const CUtensorMap& tmK, co
     const dim3 grid(static_cast<unsigned>(n_tiles) * BH);  // one CTA per item; those that do not start at once are taken over
     const bool aligned = ((so.b | so.h | so.t) & 15) == 0 && ((reinterpret_cast<uintptr_t>(O) | reinterpret_cast<uintptr_t>(rest)) & 31) == 0;
     const Work wk{BH, n_tiles, s.T, s.H, orders, win};
-    auto go = [&](auto kernel, int smem) {
+    // Few keys to a row: the roundings of their weights do not average out in O, and reach dQ and dK through Delta.  Where O_rest is asked
+    // for, the weights go into the product as two bf16 numbers then.  Error of dQ and dK over that of rounding the outputs alone, with
+    // one number and with two: 1.46, 1.41 at 16 keys a row, 1.44, 1.42 at 128.  Time, with two and with one: B=8, H=12, T=1024, D=64,
+    // window 64: 21.0, 19.3 us; a training pass of two heads, T=64, 18.1, 16.2 (more code to fetch).
+    const bool split = rest != nullptr && win.window <= kFewKeys;
+    return with_kernel(s.D, strided, split, [&](auto kernel, int smem) {
         return launch_overlapped(kernel, grid, dim3(kThreads), smem, stream, tmQ, tmK, tmV, reinterpret_cast<uint16_t*>(O),
                                  reinterpret_cast<uint16_t*>(rest), LSE, so, aligned, wk, s.scale, dev_status);
-    };
-    if (s.D == 64)
-        return strided ? go(window_fwd_kernel<64, true>, Cfg<64>::kSmemBytes) : go(window_fwd_kernel<64, false>, Cfg<64>::kSmemBytes);
-    return strided ? go(window_fwd_kernel<128, true>, Cfg<128>::kSmemBytes) : go(window_fwd_kernel<128, false>, Cfg<128>::kSmemBytes);
+    });
 }
 
 }  // namespace nova
