@@ -65,7 +65,8 @@ int nova_rope_bwd(const void* dQ_out, const void* dK_out, void* dQ, void* dK, co
  *                     on it stays, up to `low` turns it is divided by factor, between the two
  *                     inv_freq * (r + (1 - r) / factor) with r = (n - low) / (high - low)
  *   NOVA_ROPE_YARN    the same with r linear in the pair's number i between those at which n is high and low, rounded down and
- *                     up (Peng et al., "YaRN", 2023), and amplitude = 0.1 ln(factor) + 1
+ *                     up and kept within 0 and rotary - 1 (Peng et al., "YaRN", 2023); where every frequency turns `high` times
+ *                     all stay, where none turns more than `low` times all are divided; amplitude = 0.1 ln(factor) + 1
  * Writes rotary / 2 numbers to inv_freq and the amplitude (1 but for YARN) to *amplitude, both on the host.  Returns
  * NOVA_ATTN_OK, NOVA_ATTN_ERR_NULL, or NOVA_ATTN_ERR_SHAPE: rotary odd or < 2 (< 4 for BASE), base <= 1, an unknown kind; where the
  * kind uses them factor < 1, original < 1, low <= 0 or high <= low; anything not finite.

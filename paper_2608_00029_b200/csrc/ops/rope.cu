@@ -278,13 +278,14 @@ int nova_rope_frequencies(float* inv_freq, float* amplitude, int rotary, double 
     auto pair_of = [&](double n) { return R * std::log(original / (n * kTwoPi)) / (2.0 * std::log(base)); };
     const double at_high = bands ? std::fmax(std::floor(pair_of(high)), 0.0) : 0.0;
     double at_low = bands ? std::fmin(std::ceil(pair_of(low)), R - 1.0) : 0.0;
-    if (at_low == at_high) at_low += 1e-3;
+    if (at_low <= at_high) at_low = at_high + 1e-3;  // (where the bounds leave no pair between them)
+    const bool none_stays = kind == NOVA_ROPE_YARN && original <= low * kTwoPi;  // the fastest turns `low` times at most
     for (int i = 0; i < rotary / 2; ++i) {
         const double f = std::pow(base, -2.0 * i / R);
         double r = 1.0;  // the part that stays
         if (kind == NOVA_ROPE_LINEAR) r = 0.0;
         if (kind == NOVA_ROPE_BANDS) r = (original * f / kTwoPi - low) / (high - low);
-        if (kind == NOVA_ROPE_YARN) r = 1.0 - (i - at_high) / (at_low - at_high);
+        if (kind == NOVA_ROPE_YARN) r = none_stays ? 0.0 : 1.0 - (i - at_high) / (at_low - at_high);
         r = r < 0.0 ? 0.0 : r > 1.0 ? 1.0 : r;
         inv_freq[i] = static_cast<float>(r == 1.0 ? f : f * (r + (1.0 - r) / factor));
     }
