@@ -40,8 +40,9 @@ extern "C" {
  * Forward.
  *   Q, K, V : in,  bf16
  *   O       : out, bf16
- *   O_rest  : out, bf16 with the strides of O, or NULL: what the rounding took from O (O + O_rest is the result to 16 bits), for
- *             nova_window_bwd_preprocess
+ *   O_rest  : out, bf16 with the strides of O, or NULL: what the rounding took from O (O + O_rest is the sum before it was rounded,
+ *             to 16 bits), for nova_window_bwd_preprocess.  A call with O_rest whose rows keep at most 64 keys (window + sinks, or T)
+ *             takes more exact weights, so that its O and a call's without O_rest may differ by a rounding
  *   LSE     : out, fp32 [B,H,T] contiguous, natural-log log-sum-exp of the kept scaled scores
  */
 int nova_window_fwd(const void* Q, const void* K, const void* V, void* O, void* O_rest, float* LSE, int B, int H, int H_kv,

@@ -22,6 +22,7 @@
 // there is no shared memory to stage it in, and no need to wait for it.
 //
 // 192 threads: warp 0 TMA producer, warp 1 UMMA issuer, warps 2-5 softmax.  Items are handed out dynamically (WorkRing).
+#include <algorithm>
 #include <type_traits>
 
 #include "../api.h"
@@ -35,7 +36,7 @@ constexpr int kThreads = 192;
 constexpr int kTmemCols = 256;
 constexpr int kStep = kKeyStep;
 constexpr float kRescaleThreshold = 8.0f;  // log2 units
-constexpr int kFewKeys = 64;  // (see launch_window_fwd)
+constexpr int kFewKeys = 64;  // that a row keeps, window and sinks (see launch_window_fwd)
 
 template <int D>
 struct Cfg {
@@ -534,7 +535,7 @@ cudaError_t launch_window_fwd(const CUtensorMap& tmQ, const CUtensorMap& tmK, co
     // for, the weights go into the product as two bf16 numbers then.  Error of dQ and dK over that of rounding the outputs alone, with
     // one number and with two: 1.46, 1.41 at 16 keys a row, 1.44, 1.42 at 128.  Time, with two and with one: B=8, H=12, T=1024, D=64,
     // window 64: 21.0, 19.3 us; a training pass of two heads, T=64, 18.1, 16.2 (more code to fetch).
-    const bool split = rest != nullptr && win.window <= kFewKeys;
+    const bool split = rest != nullptr && std::min<long long>(static_cast<long long>(win.window) + win.sinks, s.T) <= kFewKeys;
     return with_kernel(s.D, strided, split, [&](auto kernel, int smem) {
         return launch_overlapped(kernel, grid, dim3(kThreads), smem, stream, tmQ, tmK, tmV, reinterpret_cast<uint16_t*>(O),
                                  reinterpret_cast<uint16_t*>(rest), LSE, so, aligned, wk, s.scale, dev_status);

@@ -74,3 +74,15 @@ def test_weights_of_two_numbers(window, sinks, D, fused):
     e = (s - s.amax(-1, keepdim=True)).exp()
     one = (e.to(torch.bfloat16).double() @ vx) / e.sum(-1, keepdim=True)
     assert ((one - want).abs() > bound).double().mean() > 0.5, "the bound would not tell weights of one number"
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(32, 150), (64, 1), (40, 2**31 - 1), (1, 64)])
+def test_rows_that_keep_many_keys_have_weights_of_one_number(window, sinks, D):
+    """Sinks count as the window does: with more than 64 keys to a row O has the same bits whether O_rest is asked for or not."""
+    _, nw = _libs()
+    p = Problem(2, 4, 2, 300, D, False, seed=D + window)
+    nw.nova_window_fwd(p.q, p.k, p.v, p.o, p.lse, p.scale, window, sinks)
+    o, lse = p.o.clone(), p.lse.clone()
+    nw.nova_window_fwd(p.q, p.k, p.v, p.o, p.lse, p.scale, window, sinks, O_rest=p.rest)
+    assert torch.equal(p.o, o) and torch.equal(p.lse, lse)
