@@ -403,6 +403,12 @@ struct View {
     }
 };
 
+// Do two views of one shape have the same strides?  (That of a dimension of size one does not count.)
+bool same_places(const View& x, const View& y) {
+    return (x.n[0] == 1 || x.st.batch == y.st.batch) && (x.n[1] == 1 || x.st.head == y.st.head) &&
+           (x.n[2] == 1 || x.st.token == y.st.token);
+}
+
 float* f32_on(PyObject* o, const char* name, const OnDevice& dev, at::IntArrayRef want) {
     float* p = f32(o, name, want);
     dev.same(THPVariable_Unpack(o), name);
@@ -456,8 +462,7 @@ int window_fwd(Args a) {  // Q K V O O_rest LSE scale window sinks stream
     void* rest = nullptr;
     if (a[4] != Py_None) {
         const View r(a[4], "O_rest", dev, B, H, T, D);
-        if (r.st.batch != o.st.batch || r.st.head != o.st.head || r.st.token != o.st.token)
-            raise(PyExc_ValueError, "O_rest must have the strides of O");
+        if (!same_places(r, o)) raise(PyExc_ValueError, "O_rest must have the strides of O");
         rest = r.ptr;
     }
     float* lse = f32_on(a[5], "LSE", dev, {B, H, T});
@@ -477,8 +482,7 @@ int window_preprocess(Args a) {  // O O_rest dO Delta stream
     void* rest = nullptr;
     if (a[1] != Py_None) {
         const View r(a[1], "O_rest", dev, B, H, T, D);
-        if (r.st.batch != o.st.batch || r.st.head != o.st.head || r.st.token != o.st.token)
-            raise(PyExc_ValueError, "O_rest must have the strides of O");
+        if (!same_places(r, o)) raise(PyExc_ValueError, "O_rest must have the strides of O");
         rest = r.ptr;
     }
     const View g(a[2], "dO", dev, B, H, T, D);

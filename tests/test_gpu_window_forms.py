@@ -86,3 +86,38 @@ def test_rows_that_keep_many_keys_have_weights_of_one_number(window, sinks, D):
     o, lse = p.o.clone(), p.lse.clone()
     nw.nova_window_fwd(p.q, p.k, p.v, p.o, p.lse, p.scale, window, sinks, O_rest=p.rest)
     assert torch.equal(p.o, o) and torch.equal(p.lse, lse)
+
+
+def test_rest_in_another_layout_of_the_same_places():
+    """One head: [B,1,T,D] and a view of [B,T,1,D] have the same elements at the same places, whatever the stride of the one head."""
+    _, nw = _libs()
+    for D in (64, 128):
+        p = Problem(2, 1, 1, 200, D, False, seed=D, pad=0)
+        rest = torch.empty((2, 200, 1, D), dtype=torch.bfloat16, device=p.o.device).transpose(1, 2)
+        assert rest.stride() != p.o.stride()
+        nw.nova_window_fwd(p.q, p.k, p.v, p.o, p.lse, p.scale, 50, 2, O_rest=rest)
+        nw.nova_window_bwd_preprocess(p.o, rest, p.do, p.delta)
+        delta = p.delta.clone()
+        nw.nova_window_fwd(p.q, p.k, p.v, p.o, p.lse, p.scale, 50, 2, O_rest=p.rest)
+        nw.nova_window_bwd_preprocess(p.o, p.rest, p.do, p.delta)
+        assert torch.equal(rest, p.rest) and torch.equal(delta, p.delta)
+        one = torch.empty((1, 4, 1, D), dtype=torch.bfloat16, device=p.o.device)  # one token: neither its stride nor the sequence's
+        wide = torch.empty((3, 4, 9, D), dtype=torch.bfloat16, device=p.o.device)[:1, :, :1]
+        with pytest.raises(ValueError):  # other heads' places
+            nw.nova_window_fwd(one, one, one, one.clone(), torch.empty((1, 4, 1), device=p.o.device), 0.1, 4, O_rest=wide)
+
+
+def test_rotation_in_place_through_another_view():
+    """In place is the same elements at the same places: the stride of a single head or sequence does not count."""
+    from paper_2608_00029_b200 import nova_rope as nr
+    g = torch.Generator().manual_seed(3)
+    x = torch.randn((1, 1, 50, 64), generator=g).to(torch.bfloat16).to("cuda:0")
+    freq, _ = nr.nova_rope_frequencies(64)
+    freq = freq.to("cuda:0")
+    want = torch.empty_like(x)
+    nr.nova_rope_fwd(x, None, want, None, freq)
+    other = x.as_strided((1, 1, 50, 64), (64, 64, 64, 1))
+    nr.nova_rope_fwd(x, None, other, None, freq)
+    assert torch.equal(x, want)
+    with pytest.raises(_libs()[0].NovaAttnError):  # other places
+        nr.nova_rope_fwd(x[:, :, :25], None, x.as_strided((1, 1, 25, 64), (3200, 3200, 128, 1)), None, freq)
