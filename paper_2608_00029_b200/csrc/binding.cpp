@@ -447,10 +447,13 @@ int rope(Args a) {  // Q K Q_out K_out inv_freq positions interleaved amplitude 
     const float amplitude = real(a[7]);
     const int backward = truth(a[8]);
     void* st = dev.stream(a[9]);
+    // in place through another view of the same places: the library wants one set of strides
+    const nova_attn_strides& qo_st = qo.ptr == q.ptr && same_places(q, qo) ? q.st : qo.st;
+    const nova_attn_strides& ko_st = ko.ptr == k.ptr && same_places(k, ko) ? k.st : ko.st;
     return without_gil([&] {
         return (backward ? nova_rope_bwd : nova_rope_fwd)(q.ptr, with_k ? k.ptr : nullptr, qo.ptr, with_k ? ko.ptr : nullptr,
                                                           static_cast<const float*>(data(f)), pos, B, H, k.n[1], T, D, rotary,
-                                                          interleaved, amplitude, pos_stride, &q.st, &k.st, &qo.st, &ko.st, st);
+                                                          interleaved, amplitude, pos_stride, &q.st, &k.st, &qo_st, &ko_st, st);
     });
 }
 

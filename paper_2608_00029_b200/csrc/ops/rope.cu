@@ -190,10 +190,8 @@ int rope(const void* Q, const void* K, void* Qo, void* Ko, const float* inv_freq
         if (int rc = check_strides(k, D, &a.sin[1])) return rc;
         if (int rc = check_strides(ko, D, &a.sout[1])) return rc;
     }
-    auto same = [&](const TensorStrides& x, const TensorStrides& y, int heads) {  // (that of a dimension of size one is not used)
-        return (B == 1 || x.b == y.b) && (heads == 1 || x.h == y.h) && (T == 1 || x.t == y.t);
-    };
-    if ((Q == Qo && !same(a.sin[0], a.sout[0], H)) || (K && K == Ko && !same(a.sin[1], a.sout[1], H_kv))) return NOVA_ATTN_ERR_SHAPE;
+    auto same = [](const TensorStrides& x, const TensorStrides& y) { return x.b == y.b && x.h == y.h && x.t == y.t; };
+    if ((Q == Qo && !same(a.sin[0], a.sout[0])) || (K && K == Ko && !same(a.sin[1], a.sout[1]))) return NOVA_ATTN_ERR_SHAPE;
     DeviceState* st = nullptr;
     if (int rc = device_state(&st)) return rc;
 
