@@ -39,8 +39,8 @@ extern "C" {
  * Requirements: D a multiple of 8 up to 1024, rotary even, 2 <= rotary <= D, B * T <= 2^30, H + H_kv <= 2^24, position_stride >= 0;
  * strides as in the strided calls of nova_attn.h (multiples of 8, token >= D, head and batch >= 8, below 2^39); tensors 16-byte
  * aligned, inv_freq and positions 4-byte; amplitude finite.  Errors (checked on the host before any launch):
- * NOVA_ATTN_ERR_NULL, NOVA_ATTN_ERR_SHAPE (sizes, rotary, strides), NOVA_ATTN_ERR_ALIGNMENT, NOVA_ATTN_ERR_SCALE (amplitude), NOVA_ATTN_ERR_UNSUPPORTED (device is not sm_100),
- * NOVA_ATTN_ERR_CUDA.
+ * NOVA_ATTN_ERR_NULL, NOVA_ATTN_ERR_SHAPE (sizes, rotary, strides), NOVA_ATTN_ERR_ALIGNMENT, NOVA_ATTN_ERR_SCALE (amplitude),
+ * NOVA_ATTN_ERR_UNSUPPORTED (device is not sm_100), NOVA_ATTN_ERR_CUDA.
  */
 int nova_rope_fwd(const void* Q, const void* K, void* Q_out, void* K_out, const float* inv_freq, const int* positions,
                   int B, int H, int H_kv, int T, int D, int rotary, int interleaved, float amplitude,

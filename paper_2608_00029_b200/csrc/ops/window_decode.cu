@@ -350,9 +350,9 @@ DecodePlan decode_plan(int B, int H, int H_kv, int T_max, int D, int window, int
     constexpr int kLeast = kWarps * kTile;
     auto rounded = [](long long chunk) { return (chunk + kLeast - 1) / kLeast * kLeast; };
     // Where it leaves no run longer than 1280 keys: as many runs to a row as leave no more CTAs than the GPU holds at once, so that all start
-    // together and the last is done when the first is (us against eight CTAs to an SM: B=16, H=32 on 8, D=128, 1024 keys: 14.8, 20.4; B=8, 4096 keys: 24.9, 31.2;
-    // B=1, 8192 keys: 11.9, 15.7; B=8, H=12, D=64, 1024 keys: 9.2, 11.2).  In clusters if they can be a few longer runs: B=4, H=32 on
-    // 8, D=128, 2048 keys: 11.4 with 8 to a row, 12.2 with 11 and a kernel to join them.
+    // together and the last is done when the first is (us against eight CTAs to an SM: B=16, H=32 on 8, D=128, 1024 keys: 14.8, 20.4; B=8,
+    // 4096 keys: 24.9, 31.2; B=1, 8192 keys: 11.9, 15.7; B=8, H=12, D=64, 1024 keys: 9.2, 11.2).  In clusters if they can be a few longer
+    // runs: B=4, H=32 on 8, D=128, 2048 keys: 11.4 with 8 to a row, 12.2 with 11 and a kernel to join them.
     // From half of those CTAs on that is one run to a row.  H=32 on 8, D=128, 1024 keys, with one run, with three and with six: B=28 (224 of
     // 444 CTAs) 27.6, 28.9, 28.8, B=36 29.8, 32.1, 35.0, B=55 37.4, 45.5, 47.4; lengths up to 1024, where some rows end early, B=28 21.9,
     // 17.2, 17.7, B=36 23.8, 21.2, 21.1, B=55 26.5, 29.0, 28.5.

@@ -66,9 +66,9 @@ KvParts kv_parts(int BH, int T, int D, const Window& win) {
     // Parts of tiles whose longest list is the first, the shortest the last.  One count for all of them, so that an item's tile is found by
     // a division, and no more than the shortest list has steps: the sequence's last tile has `group` of them or twice that, so without
     // shared heads nothing is cut, or in two, whatever is said below.  With counts by ranges of tiles the look-up cost more than that
-    // mostly gave.  Backward (us), one count and ranges: H=2, T=64, D=64 7.4, 8.1; B=8, H=12, T=1024, D=64 54, 58; H=16 on 2, T=768, D=128 31,
-    // 35; H=2, T=4097, window 1024, D=128 27, 40; where it gave, whole triangles on few heads: H=1, T=8193, D=128 140, 124; H=4 on 2,
-    // T=1025, D=128 30, 23.
+    // mostly gave.  Backward (us), one count and ranges: H=2 on 1, T=64, window 16, D=64 7.4, 8.1; B=8, H=12, T=1024, window 256, D=64 54, 58;
+    // H=16 on 2, T=768, window 475, D=128 31, 35; H=2, T=4097, window 1024, D=128 27, 40; where it gave, whole triangles on few heads: H=1,
+    // T=8193, D=128 140, 124; H=4 on 2, T=1025, D=128 30, 23.
     auto cut = [&](int first, int last, long long most) -> int {
         const long long n = (list(first) + most - 1) / most;
         return static_cast<int>(std::max(1ll, std::min(n, list(last))));
@@ -81,8 +81,8 @@ KvParts kv_parts(int BH, int T, int D, const Window& win) {
     const long long rest = static_cast<long long>(p.n_tiles - p.sink_tiles) * BH;
     if (D == 128) {
         // dQ comes behind and fills up what these leave: as far as `cut` goes no part longer than an SM's share of the steps of both (a
-        // step of dQ takes two thirds of one here).  B=2, H=12 on 4, T=8192, window 1024, 4 sinks, a list of 384 steps, a share of 349: 419 us in one item,
-        // 370 in 2; H=12 on 4, T=4096, window 300, 1 sink, 192 and 38: 220, 61 in 6, 66 in 16; H=16 on 4, T=4096, window 512, all lists of
+        // step of dQ takes two thirds of one here).  B=2, H=12 on 4, T=8192, window 1024, 4 sinks, a list of 384 steps, a share of 349:
+        // 419 us in one item, 370 in 2; H=12 on 4, T=4096, window 300, 1 sink, 192 and 38: 220, 61 in 6, 66 in 16; H=16 on 4, T=4096, window 512, all lists of
         // 40, 55: 80, 93 in 2; H=16 on 2, T=768, window 475, 1 sink, 96 and 80, 8: 104, 31 in 12 and 8, 35 in 6 and 6.  Parts without
         // sinks, which come later and are more, may be a third longer: H=16 on 4, T=1024, window 1024, 64 steps, 12: 34 in 4, 40 in 5.
         const long long most = std::max(std::min(few, 8ll), 5 * total / (3 * kSms));
